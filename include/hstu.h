@@ -363,6 +363,180 @@ hstu_status_t hstu_proj_in_bwd(const hstu_problem_t* p, int32_t d_model,
                                void* dx, float* dw1, float* db1,
                                void* ws, size_t ws_bytes, void* hip_stream);
 
+/* ---- Rotary positions of Q and K ----
+ * The first rot_dim features of every head (even, 2 <= rot_dim <= d_qk) turn
+ * in pairs (a, b): with m in [0, rot_dim / 2) and the angle theta =
+ * position * inv_freq[m],
+ *   a' = s (a cos theta - b sin theta),  b' = s (a sin theta + b cos theta);
+ * the other features are copied.  Pair m holds features m and m + rot_dim / 2
+ * (HSTU_ROTARY_HALVES) or 2m and 2m + 1 (HSTU_ROTARY_INTERLEAVED).  s is
+ * `amplitude`.  The angles are taken in fp64 (positions up to 2^53), the
+ * turned values in fp32, rounded once to the problem's dtype. */
+typedef enum { HSTU_ROTARY_HALVES = 0, HSTU_ROTARY_INTERLEAVED = 1 } hstu_rotary_layout_t;
+
+/* How the frequencies base^(-2 m / rot_dim) change for contexts `factor`
+ * times longer than the `original_len` positions of training (factor >= 1):
+ *   NONE    they stay;
+ *   LINEAR  all are divided by factor (positions are interpolated);
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) replaces base: the slowest
+ *           pair turns factor times slower, the fastest as before;
+ *   PARTS   a pair that turns r = original_len * f / (2 pi) times over the
+ *           original context keeps its frequency for r >= high, is divided by
+ *           factor for r <= low, and blends linearly in r between. */
+typedef enum {
+  HSTU_ROTARY_SCALE_NONE = 0,
+  HSTU_ROTARY_SCALE_LINEAR = 1,
+  HSTU_ROTARY_SCALE_BASE = 2,
+  HSTU_ROTARY_SCALE_PARTS = 3
+} hstu_rotary_scaling_t;
+
+/* inv_freq (HOST memory, rot_dim / 2 doubles) of the formulas above.
+ * original_len, low and high are read by HSTU_ROTARY_SCALE_PARTS only
+ * (original_len > 0, low < high; 1 and 32 are usual). */
+hstu_status_t hstu_rotary_frequencies(int32_t rot_dim, double base,
+                                      hstu_rotary_scaling_t scaling, double factor,
+                                      double original_len, double low, double high,
+                                      double* inv_freq);
+
+/* q_out, k_out (dense [T][h][d_qk]) = q, k (rows at q_stride / k_stride)
+ * turned by their positions.  positions: int64 [T], or NULL: the token's
+ * index in its sequence, at most n_h (the position rule of the candidates;
+ * num_targets NULL: none), for which seq_offsets is needed; otherwise
+ * seq_offsets and num_targets are not read.  Either of q and k may be NULL
+ * together with its output.  inv_freq: rot_dim / 2 doubles in device memory.
+ * p: total_tokens, num_heads, d_qk, dtype and, without positions, num_seqs
+ * matter.  Deterministic; a row's bits do not depend on the other rows. */
+hstu_status_t hstu_rotary_fwd(const hstu_problem_t* p, const int64_t* seq_offsets,
+                              const int64_t* num_targets, const int64_t* positions,
+                              const double* inv_freq, int32_t rot_dim,
+                              hstu_rotary_layout_t layout, float amplitude,
+                              const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              void* q_out, void* k_out, void* hip_stream);
+
+/* Backward of hstu_rotary_fwd: dq, dk = d_q_out, d_k_out turned back (theta
+ * negated, the same amplitude), d_q_out and d_k_out rows at the given
+ * strides, dq and dk dense. */
+hstu_status_t hstu_rotary_bwd(const hstu_problem_t* p, const int64_t* seq_offsets,
+                              const int64_t* num_targets, const int64_t* positions,
+                              const double* inv_freq, int32_t rot_dim,
+                              hstu_rotary_layout_t layout, float amplitude,
+                              const void* d_q_out, int64_t dq_stride,
+                              const void* d_k_out, int64_t dk_stride,
+                              void* dq, void* dk, void* hip_stream);
+
+/* ---- Paged cache of keys and values ----
+ * A pool of pages of page_size tokens, in device memory of the caller; user b
+ * owns the pages page_table[b][0 ..] and its token at position t lies in page
+ * page_table[b][t / page_size] at place t % page_size.  A page may belong to
+ * several users (a shared prefix), as long as none of them writes to it.
+ *   k       [num_pages][h][page_size][d_qk]
+ *   v       [num_pages][h][d_v][page_size], transposed: the attention reads
+ *           a feature's keys side by side
+ *   k_scale, v_scale  fp32 [num_pages][h][page_size] (NULL for bf16 caches)
+ *   timestamps        int64 [num_pages][page_size]
+ * A row is one token of one head; what is held of a row x is
+ *   BF16    x rounded to bf16;
+ *   INT8    code * s, s = max|x| / 127 rounded to fp32, code = x / s rounded
+ *           to the nearest integer (ties to even);
+ *   E4M3    code * s, s the smallest power of two (at most 2^119) with
+ *           max|x| <= 448 s, code = x / s rounded to the nearest 8-bit float of
+ *           4 exponent and 3 mantissa bits (no infinities, largest 448; ties
+ *           to even; larger magnitudes saturate).
+ * Codes are exact: the quotient is never rounded before its code is chosen.  A
+ * row of magnitudes below 2^-100 is held as zeros with s = 1, a row with an
+ * infinity or a NaN as zero codes with s = NaN: it reads back as NaN. */
+typedef enum {
+  HSTU_CACHE_BF16 = 0,
+  HSTU_CACHE_E4M3 = 1,
+  HSTU_CACHE_INT8 = 2
+} hstu_cache_dtype_t;
+
+typedef struct {
+  int64_t num_pages;  /* pages in the pool, in [1, 2^31 - 1]                        */
+  int32_t page_size;  /* 16, 32, 64, 128 or 256                                     */
+  int32_t max_pages;  /* columns of page_table: the most pages a user can own       */
+  hstu_cache_dtype_t dtype;
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t* timestamps;
+  const int32_t* page_table; /* [B][max_pages]; entries behind a user's last page
+                                are not read                                        */
+  const int64_t* lengths;    /* [B]: tokens in the cache                            */
+} hstu_cache_t;
+
+/* Writes rows of k and v (as in hstu_attn_fwd, in the problem's dtype, F32 or
+ * BF16) and their timestamps into the cache: token i of sequence b of the
+ * jagged batch (seq_offsets) goes to position starts[b] + i (starts NULL: i).
+ * Everything else in the pool keeps its bits.  lengths is neither read nor
+ * changed.  Positions outside [0, max_pages * page_size) and pages outside the
+ * pool are dropped.  No two tokens of a call may go to the same place.
+ * p: num_seqs, total_tokens, num_heads, d_qk, d_v, dtype matter. */
+hstu_status_t hstu_cache_write(const hstu_problem_t* p, const hstu_cache_t* c,
+                               const int64_t* seq_offsets, const int64_t* starts,
+                               const int64_t* timestamps,
+                               const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, void* hip_stream);
+
+/* Reads positions starts[b] + i, i < seq_offsets[b+1] - seq_offsets[b], of each
+ * user back into rows seq_offsets[b] + i of k, v (dense [T][h][d], in the
+ * problem's dtype: code * s in fp32, rounded once) and timestamps (int64 [T],
+ * or NULL to skip).  Positions outside [0, lengths[b]) and pages outside the
+ * pool read as zeros. */
+hstu_status_t hstu_cache_read(const hstu_problem_t* p, const hstu_cache_t* c,
+                              const int64_t* seq_offsets, const int64_t* starts,
+                              void* k, void* v, int64_t* timestamps, void* hip_stream);
+
+/* Synchronously copies lengths and the page table to the host and checks that
+ * 0 <= lengths[b] <= max_pages * page_size and that the pages of every user's
+ * first lengths[b] tokens lie in the pool; HSTU_ERR_DATA on a violation. */
+hstu_status_t hstu_cache_validate(const hstu_problem_t* p, const hstu_cache_t* c,
+                                  void* hip_stream);
+
+/* ---- Attention of drafted tokens over the cache ----
+ * The rows of the jagged batch j are drafted tokens: sequence b has L_b of
+ * them (at most max_draft <= HSTU_MAX_DRAFT, rows past it are not written),
+ * a forest given by parents [T]: the index, within the sequence, of the node
+ * that a node follows, smaller than its own, or -1 for a root (as is any
+ * other value outside [0, i)), which follows the cached tokens directly.
+ * parents NULL: all are roots, e.g. ranking candidates.  A node at depth d_i
+ * (0 for a root) sits at position p_i = n_b + d_i, n_b = lengths[b], and sees
+ * the n_b cached tokens, the nodes on its way to its root and itself:
+ *   out_i = (1/N) (sum_{j < n_b} SiLU(q_i . kc_j + rab(j - p_i, t_i - tc_j)) vc_j
+ *                + sum_{j on i's way} SiLU(q_i . k_j + rab(p_j - p_i, t_i - t_j)) v_j)
+ * with rab(x, dt) = rab_pos[N-1 + x] + rab_time[bkt(dt)], positions further
+ * back than N - 1 taking rab_pos[0].  A chain (parents i - 1) of one token or
+ * several gives the outputs that hstu_attn_fwd gives the last tokens of a
+ * sequence, but for the cache's rounding.  Cached tokens on a page outside the
+ * pool, and past max_pages * page_size, are left out.  Drafted keys and values
+ * are taken as they are (bf16); what a node does not see changes none of its
+ * bits, also infinities and NaN.
+ * p: num_seqs = B, total_tokens = T, max_seq_len = N; bf16 problems only.
+ * num_targets of j is ignored.  The cached keys are split over workgroups,
+ * the more the fewer rows there are (a rule on B, T, h, N, max_draft and
+ * max_pages alone), whose fp32 partial outputs are added in order: the call is
+ * deterministic.  ws: hstu_attn_fwd_tree_workspace_bytes bytes (0 if p, c or
+ * max_draft is invalid; c's pointers are not looked at), 256-byte aligned. */
+#define HSTU_MAX_DRAFT 1024
+size_t hstu_attn_fwd_tree_workspace_bytes(const hstu_problem_t* p, const hstu_cache_t* c,
+                                          int32_t max_draft);
+
+hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j,
+                                 const hstu_cache_t* c, const int64_t* parents,
+                                 int32_t max_draft,
+                                 const void* q, int64_t q_stride,
+                                 const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride,
+                                 void* out, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* positions[t] = base[b] + depth of drafted token t (base NULL: 0), for
+ * hstu_rotary_fwd: the p_i above.  parents and max_draft as above; seq_offsets
+ * [B+1], positions int64 [T]. */
+hstu_status_t hstu_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_t max_draft,
+                                  const int64_t* seq_offsets, const int64_t* parents,
+                                  const int64_t* base, int64_t* positions, void* hip_stream);
+
 /* ---- Stochastic Length (Eq. 4; subsequence selection and sparsity in
  * the appendix on Stochastic Length) ----
  * Shrinks a jagged batch before attention.  With L = subseq_len

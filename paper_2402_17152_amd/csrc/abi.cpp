@@ -509,9 +509,347 @@ hipError_t weight_grad(const ProjDims& d, const void* a, int64_t lda, const void
   return launch_reduce_slabs((int64_t)M * N, splits, slab, dw, s);
 }
 
+// ---- rotary positions -----------------------------------------------------
+
+hstu_status_t rotary_run(const hstu_problem_t* p, const int64_t* seq_offsets,
+                         const int64_t* num_targets, const int64_t* positions,
+                         const double* inv_freq, int32_t rot_dim, hstu_rotary_layout_t layout,
+                         float amplitude, int back, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, void* q_out, void* k_out, hipStream_t s) {
+  HSTU_TRY(check_problem(p));
+  if (rot_dim < 2 || rot_dim % 2 || rot_dim > p->d_qk)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "rot_dim must be even and in [2, d_qk] (got %d)",
+                rot_dim);
+  if (layout != HSTU_ROTARY_HALVES && layout != HSTU_ROTARY_INTERLEAVED)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "unknown rotary layout %d", (int)layout);
+  if (!inv_freq) return fail(HSTU_ERR_INVALID_ARGUMENT, "inv_freq is NULL");
+  if (!positions && !seq_offsets)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "positions and seq_offsets are both NULL");
+  if (!q && !k) return fail(HSTU_ERR_INVALID_ARGUMENT, "q and k are both NULL");
+  if (!q != !q_out || !k != !k_out)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "q and k are NULL together with their outputs only");
+  if (p->total_tokens > INT32_MAX)
+    return fail(HSTU_ERR_UNSUPPORTED, "rotary positions of more than 2^31 - 1 tokens");
+  const int64_t width = (int64_t)p->num_heads * p->d_qk;
+  if (q) HSTU_TRY(check_mat("q", q, q_stride, width, elem_size(p), p->total_tokens));
+  if (k) HSTU_TRY(check_mat("k", k, k_stride, width, elem_size(p), p->total_tokens));
+  HSTU_TRY(check_opt("q output", q_out));
+  HSTU_TRY(check_opt("k output", k_out));
+  if (p->total_tokens == 0) return ok();
+  RotaryArgs a{};
+  a.seq_offsets = seq_offsets;
+  a.num_targets = num_targets;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.total_tokens = p->total_tokens;
+  a.num_seqs = p->num_seqs;
+  a.num_heads = p->num_heads;
+  a.d = p->d_qk;
+  a.half = rot_dim / 2;
+  a.interleaved = layout == HSTU_ROTARY_INTERLEAVED;
+  a.back = back;
+  a.amplitude = amplitude;
+  a.src[0] = q;
+  a.src[1] = k;
+  a.stride[0] = q_stride;
+  a.stride[1] = k_stride;
+  a.dst[0] = q_out;
+  a.dst[1] = k_out;
+  TimedScope ts("rotary", s);
+  HSTU_HIP(launch_rotary(a, p->dtype == HSTU_BF16, s), "rotary launch");
+  return ok();
+}
+
+// ---- paged cache and the attention over it ---------------------------------
+
+// `data`: whether the pool's arrays are looked at too.
+hstu_status_t check_cache(const hstu_problem_t* p, const hstu_cache_t* c, bool data, CacheArgs* a) {
+  HSTU_TRY(check_problem(p));
+  if (!c) return fail(HSTU_ERR_INVALID_ARGUMENT, "cache is NULL");
+  if (c->dtype != HSTU_CACHE_BF16 && c->dtype != HSTU_CACHE_E4M3 && c->dtype != HSTU_CACHE_INT8)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "unknown cache dtype %d", (int)c->dtype);
+  if (c->num_pages < 1 || c->num_pages > INT32_MAX)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "num_pages must be in [1, 2^31 - 1] (got %lld)",
+                (long long)c->num_pages);
+  if (c->max_pages < 1)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "max_pages must be >= 1 (got %d)", c->max_pages);
+  int lg = 4;
+  while (lg < 8 && 1 << lg < c->page_size) lg++;
+  if (c->page_size != 1 << lg)
+    return fail(HSTU_ERR_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256 (got %d)",
+                c->page_size);
+  if (data) {
+    HSTU_TRY(check_dense("cache k", c->k, 16));
+    HSTU_TRY(check_dense("cache v", c->v, 16));
+    if (c->dtype != HSTU_CACHE_BF16) {
+      HSTU_TRY(check_dense("k_scale", c->k_scale, 16));
+      HSTU_TRY(check_dense("v_scale", c->v_scale, 16));
+    }
+    HSTU_TRY(check_dense("cache timestamps", c->timestamps, 16));
+    HSTU_TRY(check_dense("page_table", c->page_table, 4));
+  }
+  *a = CacheArgs{};
+  a->kc = c->k;
+  a->vc = c->v;
+  a->k_scale = c->k_scale;
+  a->v_scale = c->v_scale;
+  a->tc = c->timestamps;
+  a->page_table = c->page_table;
+  a->lengths = c->lengths;
+  a->num_pages = c->num_pages;
+  a->max_pages = c->max_pages;
+  a->lg_page = lg;
+  a->total_tokens = p->total_tokens;
+  a->num_seqs = p->num_seqs;
+  a->num_heads = p->num_heads;
+  a->d_qk = p->d_qk;
+  a->d_v = p->d_v;
+  return HSTU_OK;
+}
+
+int cache_kind(const hstu_cache_t* c) {
+  return c->dtype == HSTU_CACHE_BF16 ? kCacheBf16
+         : c->dtype == HSTU_CACHE_E4M3 ? kCacheE4m3
+                                       : kCacheInt8;
+}
+
+hstu_status_t check_draft(int32_t max_draft) {
+  static_assert(kMaxDraft == HSTU_MAX_DRAFT, "the header's limit is the kernels'");
+  if (max_draft < 1)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "max_draft must be >= 1 (got %d)", max_draft);
+  if (max_draft > kMaxDraft)
+    return fail(HSTU_ERR_UNSUPPORTED, "max_draft must be <= %d (got %d)", kMaxDraft, max_draft);
+  return HSTU_OK;
+}
+
+// Bytes of workspace; the arguments are checked.
+size_t tree_workspace(const hstu_problem_t*, const hstu_cache_t*, int32_t) { return kAlign; }
+
 }  // namespace
 
 extern "C" {
+
+hstu_status_t hstu_cache_write(const hstu_problem_t* p, const hstu_cache_t* c,
+                               const int64_t* seq_offsets, const int64_t* starts,
+                               const int64_t* timestamps, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, void* hip_stream) {
+  try {
+    hipStream_t s = (hipStream_t)hip_stream;
+    CacheArgs a;
+    HSTU_TRY(check_cache(p, c, true, &a));
+    if (!seq_offsets) return fail(HSTU_ERR_INVALID_ARGUMENT, "seq_offsets is NULL");
+    const int64_t T = p->total_tokens;
+    if (T > 0 && !timestamps) return fail(HSTU_ERR_INVALID_ARGUMENT, "timestamps is NULL");
+    HSTU_TRY(check_mat("k", k, k_stride, (int64_t)p->num_heads * p->d_qk, elem_size(p), T));
+    HSTU_TRY(check_mat("v", v, v_stride, (int64_t)p->num_heads * p->d_v, elem_size(p), T));
+    if (T == 0) return ok();
+    a.seq_offsets = seq_offsets;
+    a.starts = starts;
+    a.ts = timestamps;
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    TimedScope ts("cache_write", s);
+    HSTU_HIP(launch_cache(a, cache_kind(c), p->dtype == HSTU_BF16, true, s), "cache write launch");
+    return ok();
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+hstu_status_t hstu_cache_read(const hstu_problem_t* p, const hstu_cache_t* c,
+                              const int64_t* seq_offsets, const int64_t* starts, void* k, void* v,
+                              int64_t* timestamps, void* hip_stream) {
+  try {
+    hipStream_t s = (hipStream_t)hip_stream;
+    CacheArgs a;
+    HSTU_TRY(check_cache(p, c, true, &a));
+    if (!c->lengths) return fail(HSTU_ERR_INVALID_ARGUMENT, "lengths is NULL");
+    if (!seq_offsets) return fail(HSTU_ERR_INVALID_ARGUMENT, "seq_offsets is NULL");
+    if (p->total_tokens == 0) return ok();
+    HSTU_TRY(check_dense("k", k, 16));
+    HSTU_TRY(check_dense("v", v, 16));
+    a.seq_offsets = seq_offsets;
+    a.starts = starts;
+    a.k_out = k;
+    a.v_out = v;
+    a.ts_out = timestamps;
+    TimedScope ts("cache_read", s);
+    HSTU_HIP(launch_cache(a, cache_kind(c), p->dtype == HSTU_BF16, false, s), "cache read launch");
+    return ok();
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+hstu_status_t hstu_cache_validate(const hstu_problem_t* p, const hstu_cache_t* c,
+                                  void* hip_stream) {
+  try {
+    CacheArgs a;
+    HSTU_TRY(check_cache(p, c, true, &a));
+    if (!c->lengths) return fail(HSTU_ERR_INVALID_ARGUMENT, "lengths is NULL");
+    hipStream_t s = (hipStream_t)hip_stream;
+    const size_t B = (size_t)p->num_seqs, W = (size_t)c->max_pages;
+    std::vector<int64_t> len(B);
+    std::vector<int32_t> table(B * W);
+    HSTU_HIP(hipMemcpyAsync(len.data(), c->lengths, sizeof(int64_t) * B, hipMemcpyDeviceToHost, s),
+             "copy lengths");
+    HSTU_HIP(hipMemcpyAsync(table.data(), c->page_table, sizeof(int32_t) * B * W,
+                            hipMemcpyDeviceToHost, s),
+             "copy page table");
+    HSTU_HIP(hipStreamSynchronize(s), "synchronize");
+    for (size_t b = 0; b < B; b++) {
+      if (len[b] < 0 || len[b] > (int64_t)W * c->page_size)
+        return fail(HSTU_ERR_DATA, "lengths[%zu] = %lld outside [0, %lld]", b, (long long)len[b],
+                    (long long)W * c->page_size);
+      for (size_t i = 0; i < (size_t)((len[b] + c->page_size - 1) / c->page_size); i++)
+        if (table[b * W + i] < 0 || table[b * W + i] >= c->num_pages)
+          return fail(HSTU_ERR_DATA, "page_table[%zu][%zu] = %d outside the pool of %lld pages", b,
+                      i, table[b * W + i], (long long)c->num_pages);
+    }
+    return ok();
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+size_t hstu_attn_fwd_tree_workspace_bytes(const hstu_problem_t* p, const hstu_cache_t* c,
+                                          int32_t max_draft) {
+  try {
+    CacheArgs a;
+    if (check_cache(p, c, false, &a) != HSTU_OK || check_draft(max_draft) != HSTU_OK) return 0;
+    return tree_workspace(p, c, max_draft);
+  } catch (...) {
+    return 0;
+  }
+}
+
+hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j,
+                                 const hstu_cache_t* c, const int64_t* parents, int32_t max_draft,
+                                 const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, void* out, void* ws,
+                                 size_t ws_bytes, void* hip_stream) {
+  try {
+    hipStream_t s = (hipStream_t)hip_stream;
+    TreeArgs a{};
+    HSTU_TRY(check_cache(p, c, true, &a.c));
+    HSTU_TRY(check_jagged(j));
+    if (!c->lengths) return fail(HSTU_ERR_INVALID_ARGUMENT, "lengths is NULL");
+    if (p->dtype != HSTU_BF16)
+      return fail(HSTU_ERR_UNSUPPORTED, "hstu_attn_fwd_tree supports bf16 problems only");
+    HSTU_TRY(check_draft(max_draft));
+    const int64_t T = p->total_tokens;
+    if (T > (int64_t)p->num_seqs * max_draft)
+      return fail(HSTU_ERR_INVALID_ARGUMENT, "%lld drafted tokens are more than %d for each of %d",
+                  (long long)T, max_draft, p->num_seqs);
+    const int64_t H = p->num_heads;
+    HSTU_TRY(check_mat("q", q, q_stride, H * p->d_qk, 2, T));
+    HSTU_TRY(check_mat("k", k, k_stride, H * p->d_qk, 2, T));
+    HSTU_TRY(check_mat("v", v, v_stride, H * p->d_v, 2, T));
+    HSTU_TRY(check_mat("out", out, H * p->d_v, H * p->d_v, 2, T));
+    const size_t need = tree_workspace(p, c, max_draft);
+    if (!ws) return fail(HSTU_ERR_WORKSPACE, "workspace is NULL (need %zu bytes)", need);
+    if ((uintptr_t)ws % kAlign)
+      return fail(HSTU_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (ws_bytes < need)
+      return fail(HSTU_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", ws_bytes, need);
+    if (T == 0) return ok();
+    a.ja = make_args(p, j);
+    a.ja.num_targets = nullptr;
+    a.t = Tensors{q, q_stride, k, k_stride, v, v_stride};
+    a.parents = parents;
+    a.max_draft = max_draft;
+    a.d_qk = p->d_qk;
+    a.d_v = p->d_v;
+    a.out = out;
+    TimedScope ts("attn_fwd_tree", s);
+    HSTU_HIP(launch_attn_tree(a, cache_kind(c), s), "attn_fwd_tree launch");
+    return ok();
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+hstu_status_t hstu_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_t max_draft,
+                                  const int64_t* seq_offsets, const int64_t* parents,
+                                  const int64_t* base, int64_t* positions, void* hip_stream) {
+  try {
+    if (num_seqs < 1) return fail(HSTU_ERR_INVALID_ARGUMENT, "num_seqs must be >= 1");
+    if (total_tokens < 0) return fail(HSTU_ERR_INVALID_ARGUMENT, "total_tokens must be >= 0");
+    HSTU_TRY(check_draft(max_draft));
+    if (!seq_offsets) return fail(HSTU_ERR_INVALID_ARGUMENT, "seq_offsets is NULL");
+    if (total_tokens == 0) return ok();
+    if (!positions) return fail(HSTU_ERR_INVALID_ARGUMENT, "positions is NULL");
+    HSTU_HIP(launch_tree_positions(num_seqs, total_tokens, max_draft, seq_offsets, parents, base,
+                                   positions, (hipStream_t)hip_stream),
+             "tree positions launch");
+    return ok();
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+hstu_status_t hstu_rotary_frequencies(int32_t rot_dim, double base, hstu_rotary_scaling_t scaling,
+                                      double factor, double original_len, double low, double high,
+                                      double* inv_freq) {
+  if (rot_dim < 2 || rot_dim % 2)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "rot_dim must be even and >= 2 (got %d)", rot_dim);
+  if (!(base > 0.0) || std::isinf(base))
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "base must be positive and finite");
+  if (scaling < HSTU_ROTARY_SCALE_NONE || scaling > HSTU_ROTARY_SCALE_PARTS)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "unknown rotary scaling %d", (int)scaling);
+  if (!inv_freq) return fail(HSTU_ERR_INVALID_ARGUMENT, "inv_freq is NULL");
+  if (scaling != HSTU_ROTARY_SCALE_NONE && (!(factor >= 1.0) || std::isinf(factor)))
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "factor must be finite and >= 1");
+  if (scaling == HSTU_ROTARY_SCALE_BASE && rot_dim == 2)
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "a single pair has no slowest one to stretch");
+  const bool parts = scaling == HSTU_ROTARY_SCALE_PARTS;
+  if (parts && (!(original_len > 0.0) || std::isinf(original_len)))
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "original_len must be positive and finite");
+  if (parts && (!(low < high) || std::isinf(low) || std::isinf(high)))
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "low must be below high, both finite");
+  if (scaling == HSTU_ROTARY_SCALE_BASE)
+    base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  for (int m = 0; m < rot_dim / 2; m++) {
+    double f = std::pow(base, -2.0 * m / rot_dim);
+    if (scaling == HSTU_ROTARY_SCALE_LINEAR) f /= factor;
+    if (parts) {
+      const double turns = original_len * f / 6.283185307179586;
+      const double keep = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+      f = keep * f + (1.0 - keep) * f / factor;
+    }
+    inv_freq[m] = f;
+  }
+  return ok();
+}
+
+hstu_status_t hstu_rotary_fwd(const hstu_problem_t* p, const int64_t* seq_offsets,
+                              const int64_t* num_targets, const int64_t* positions,
+                              const double* inv_freq, int32_t rot_dim, hstu_rotary_layout_t layout,
+                              float amplitude, const void* q, int64_t q_stride, const void* k,
+                              int64_t k_stride, void* q_out, void* k_out, void* hip_stream) {
+  try {
+    return rotary_run(p, seq_offsets, num_targets, positions, inv_freq, rot_dim, layout, amplitude,
+                      0, q, q_stride, k, k_stride, q_out, k_out, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
+
+hstu_status_t hstu_rotary_bwd(const hstu_problem_t* p, const int64_t* seq_offsets,
+                              const int64_t* num_targets, const int64_t* positions,
+                              const double* inv_freq, int32_t rot_dim, hstu_rotary_layout_t layout,
+                              float amplitude, const void* d_q_out, int64_t dq_stride,
+                              const void* d_k_out, int64_t dk_stride, void* dq, void* dk,
+                              void* hip_stream) {
+  try {
+    return rotary_run(p, seq_offsets, num_targets, positions, inv_freq, rot_dim, layout, amplitude,
+                      1, d_q_out, dq_stride, d_k_out, dk_stride, dq, dk, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
+  }
+}
 
 // ---- Stochastic Length (Eq. 4) ----------------------------------------
 

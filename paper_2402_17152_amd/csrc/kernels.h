@@ -271,4 +271,66 @@ hipError_t launch_gather_rows(const void* src, int64_t src_stride, int64_t row_b
                               const int64_t* index, const int64_t* count, int64_t max_rows,
                               void* dst, int64_t dst_stride, hipStream_t s);
 
+// ---- rotary positions ----
+struct RotaryArgs {
+  const int64_t* seq_offsets;  // read where positions is null
+  const int64_t* num_targets;  // may be null
+  const int64_t* positions;    // may be null
+  const double* inv_freq;      // [half]
+  int64_t total_tokens;
+  int32_t num_seqs, num_heads, d;
+  int32_t half;                // pairs a head turns
+  int32_t interleaved, back;   // back: by the negated angles
+  float amplitude;
+  const void* src[2];          // rows of Q and K, either may be null
+  int64_t stride[2];           // elements
+  void* dst[2];                // dense
+  int32_t per;                 // tokens per workgroup (set by the launcher)
+};
+hipError_t launch_rotary(RotaryArgs a, int is_bf16, hipStream_t s);
+
+// ---- paged cache ----
+enum { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2 };
+struct CacheArgs {
+  // the cache
+  void* kc;
+  void* vc;
+  float* k_scale;
+  float* v_scale;
+  int64_t* tc;
+  const int32_t* page_table;
+  const int64_t* lengths;
+  int64_t num_pages;
+  int32_t max_pages, lg_page;
+  // rows written, or read back
+  const int64_t* seq_offsets;
+  const int64_t* starts;  // may be null
+  const void* k;
+  const void* v;
+  int64_t k_stride, v_stride;
+  const int64_t* ts;
+  void* k_out;
+  void* v_out;
+  int64_t* ts_out;  // may be null
+  int64_t total_tokens;
+  int32_t num_seqs, num_heads, d_qk, d_v;
+  int64_t items;  // set by the launcher
+};
+hipError_t launch_cache(CacheArgs a, int kind, int is_bf16, bool write, hipStream_t s);
+
+// ---- attention of drafted tokens over the cache ----
+constexpr int kMaxDraft = 1024;
+struct TreeArgs {
+  JaggedArgs ja;  // of the drafted tokens
+  Tensors t;
+  CacheArgs c;    // the cache's fields only
+  const int64_t* parents;  // may be null
+  int32_t max_draft, d_qk, d_v;
+  void* out;
+};
+hipError_t launch_attn_tree(const TreeArgs& a, int kind, hipStream_t s);
+hipError_t launch_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_t max_draft,
+                                 const int64_t* seq_offsets, const int64_t* parents,
+                                 const int64_t* base, int64_t* positions, hipStream_t s);
+
 }  // namespace hstu

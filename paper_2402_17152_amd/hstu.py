@@ -31,7 +31,10 @@ EXPORTED = ("hstu_workspace_bytes", "hstu_attn_fwd", "hstu_attn_bwd", "hstu_laye
             "hstu_proj_out_fwd", "hstu_proj_out_bwd", "hstu_proj_in_bwd",
             "hstu_sl_subseq_len", "hstu_sl_keep_numerator", "hstu_sl_workspace_bytes",
             "hstu_stochastic_length", "hstu_gather_rows", "hstu_sl_sparsity",
-            "hstu_attn_fwd_noalloc")
+            "hstu_attn_fwd_noalloc",
+            "hstu_rotary_frequencies", "hstu_rotary_fwd", "hstu_rotary_bwd",
+            "hstu_cache_write", "hstu_cache_read", "hstu_cache_validate",
+            "hstu_attn_fwd_tree_workspace_bytes", "hstu_attn_fwd_tree", "hstu_tree_positions")
 
 
 class Problem(ctypes.Structure):
@@ -47,6 +50,14 @@ class Jagged(ctypes.Structure):
                 ("rab_time", ctypes.c_void_p)]
 
 
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("timestamps", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
+
+
 class HstuError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -59,7 +70,8 @@ def _load():
     lib = ctypes.CDLL(LIB_PATH)
     P, i32, i64, sz, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                             ctypes.c_float)
-    PP, PJ = ctypes.POINTER(Problem), ctypes.POINTER(Jagged)
+    PP, PJ, PC = (ctypes.POINTER(Problem), ctypes.POINTER(Jagged), ctypes.POINTER(CacheDesc))
+    f64 = ctypes.c_double
     sig = {
         "hstu_workspace_bytes": (sz, [PP]),
         "hstu_attn_fwd": (i32, [PP, PJ, P, i64, P, i64, P, i64, P, P, sz, P]),
@@ -96,6 +108,15 @@ def _load():
         "hstu_proj_out_fwd": (i32, [PP, i32, P, i64, P, P, P, P, P]),
         "hstu_proj_out_bwd": (i32, [PP, i32, P, i64, P, P, P, P, P, P, sz, P]),
         "hstu_proj_in_bwd": (i32, [PP, i32, P, i64, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "hstu_rotary_frequencies": (i32, [i32, f64, i32, f64, f64, f64, f64, P]),
+        "hstu_rotary_fwd": (i32, [PP, P, P, P, P, i32, i32, f32, P, i64, P, i64, P, P, P]),
+        "hstu_rotary_bwd": (i32, [PP, P, P, P, P, i32, i32, f32, P, i64, P, i64, P, P, P]),
+        "hstu_cache_write": (i32, [PP, PC, P, P, P, P, i64, P, i64, P]),
+        "hstu_cache_read": (i32, [PP, PC, P, P, P, P, P, P]),
+        "hstu_cache_validate": (i32, [PP, PC, P]),
+        "hstu_attn_fwd_tree_workspace_bytes": (sz, [PP, PC, i32]),
+        "hstu_attn_fwd_tree": (i32, [PP, PJ, PC, P, i32, P, i64, P, i64, P, i64, P, P, sz, P]),
+        "hstu_tree_positions": (i32, [i32, i64, i32, P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -540,6 +561,290 @@ def hstu_sl_sparsity(seq_offsets_host, max_seq_len):
     _check(lib.hstu_sl_sparsity(len(offs) - 1, offs.ctypes.data_as(ctypes.c_void_p),
                                 int(max_seq_len), ctypes.byref(sp), ctypes.byref(s2)))
     return sp.value, s2.value
+
+
+# ------------------------------------------------ rotary positions
+
+HSTU_ROTARY_HALVES, HSTU_ROTARY_INTERLEAVED = 0, 1
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def _array(name, t, dtype, count=None):
+    """Data pointer of a dense device array argument (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{name} must have {count} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _offsets(seq_offsets):
+    """(pointer, number of sequences) of an offsets array."""
+    ptr = _array("seq_offsets", seq_offsets, torch.int64)
+    if seq_offsets.numel() < 2:
+        raise ValueError("seq_offsets needs an entry for each sequence and one more")
+    return ptr, seq_offsets.numel() - 1
+
+
+def _rows(name, t, shape, dtype):
+    """Row stride of a [T, h, d] view of the given shape and dtype."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 or (shape[1] > 1 and st[1] != shape[2]):
+        raise ValueError(f"{name}: rows must be [h][d] contiguous")
+    # a single row, or none, has no stride to speak of
+    return st[0] if shape[0] > 1 else max(st[0], shape[1] * shape[2])
+
+
+def _dense_out(name, out, like, shape, dtype):
+    if out is None:
+        return like.new_empty(shape, dtype=dtype)
+    if out.dtype != dtype or out.shape != torch.Size(shape) or not out.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {tuple(shape)} of {dtype}")
+    return out
+
+
+def _on_device(*tensors):
+    """The launches go to the current device: every array has to lie there."""
+    device = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != device):
+            raise ValueError(f"an array is on {t.device}, the current device is cuda:{device}")
+
+
+def hstu_rotary_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, original_len=0.0,
+                            low=1.0, high=32.0):
+    """Inverse frequencies (numpy float64 [rot_dim / 2], host); scaling: "none",
+    "linear", "base" or "parts" (see include/hstu.h)."""
+    out = np.empty(max(int(rot_dim) // 2, 0), dtype=np.float64)
+    _check(lib.hstu_rotary_frequencies(int(rot_dim), float(base), ROTARY_SCALINGS[scaling],
+                                       float(factor), float(original_len), float(low),
+                                       float(high), out.ctypes.data_as(ctypes.c_void_p)))
+    return out
+
+
+def _rotary(call, q, k, inv_freq, seq_offsets, num_targets, positions, interleaved, amplitude,
+            out, stream):
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("q and k are both None")
+    if one.dim() != 3:
+        raise ValueError("expected a [T, h, d] tensor")
+    shape, dtype = one.shape, one.dtype
+    T, H, d = shape
+    code = _dtype_code(one)
+    qs, ks = (0 if t is None else _rows(n, t, shape, dtype) for n, t in (("q", q), ("k", k)))
+    freq = _array("inv_freq", inv_freq, torch.float64)
+    pos = _array("positions", positions, torch.int64, T)
+    offs, B = (None, 1) if seq_offsets is None else _offsets(seq_offsets)
+    nt = _array("num_targets", num_targets, torch.int64, B)
+    qo, ko = (None, None) if out is None else out
+    qo = None if q is None else _dense_out("q output", qo, q, shape, dtype)
+    ko = None if k is None else _dense_out("k output", ko, k, shape, dtype)
+    _on_device(q, k, inv_freq, positions, seq_offsets, num_targets, qo, ko)
+    p = Problem(B, T, 1, H, d, d, 1, code)
+    _check(call(ctypes.byref(p), offs, nt, pos, freq, 2 * inv_freq.numel(),
+                1 if interleaved else 0, amplitude, _ptr(q), qs, _ptr(k), ks, _ptr(qo), _ptr(ko),
+                _stream(stream)))
+    return qo, ko
+
+
+def hstu_rotary_fwd(q, k, inv_freq, seq_offsets=None, num_targets=None, positions=None,
+                    interleaved=False, amplitude=1.0, out=None, stream=None):
+    """(q', k') dense [T, h, d]: the first 2 * inv_freq.numel() features of each
+    head turned by position * inv_freq (float64, device).  Either of q and k may
+    be None.  Positions: given, or the index in the sequence (see
+    include/hstu.h)."""
+    return _rotary(lib.hstu_rotary_fwd, q, k, inv_freq, seq_offsets, num_targets, positions,
+                   interleaved, amplitude, out, stream)
+
+
+def hstu_rotary_bwd(d_q_out, d_k_out, inv_freq, seq_offsets=None, num_targets=None,
+                    positions=None, interleaved=False, amplitude=1.0, out=None, stream=None):
+    """(dq, dk) for the gradients of hstu_rotary_fwd's outputs."""
+    return _rotary(lib.hstu_rotary_bwd, d_q_out, d_k_out, inv_freq, seq_offsets, num_targets,
+                   positions, interleaved, amplitude, out, stream)
+
+
+# ------------------------------------------------ paged cache
+
+HSTU_CACHE_BF16, HSTU_CACHE_E4M3, HSTU_CACHE_INT8 = 0, 1, 2
+_CACHE_CODES = {torch.bfloat16: HSTU_CACHE_BF16, torch.float8_e4m3fn: HSTU_CACHE_E4M3,
+                torch.int8: HSTU_CACHE_INT8}
+
+
+class PagedCache:
+    """The device arrays of a paged cache (hstu_cache_t in include/hstu.h):
+    k [pages, h, page, d_qk], v [pages, h, d_v, page] of bfloat16,
+    float8_e4m3fn or int8, k_scale and v_scale [pages, h, page] (None for
+    bfloat16), timestamps [pages, page], page_table [B, max_pages] int32,
+    lengths [B] int64.  The arrays are the caller's; they are changed in place,
+    never exchanged: other arrays are another PagedCache."""
+
+    __slots__ = ("_arrays", "_desc", "_shape")
+
+    def __init__(self, k, v, timestamps, page_table, lengths, k_scale=None, v_scale=None):
+        kind = _CACHE_CODES.get(k.dtype)
+        if kind is None or v.dtype != k.dtype:
+            raise TypeError(f"a cache of {k.dtype} and {v.dtype} is not supported")
+        if k.dim() != 4 or v.dim() != 4 or page_table.dim() != 2:
+            raise ValueError("k and v have four dimensions, page_table has two")
+        pages, heads, page, d_qk = k.shape
+        d_v = v.shape[2]
+        if v.shape != (pages, heads, d_v, page):
+            raise ValueError(f"v must be {(pages, heads, d_v, page)}, got {tuple(v.shape)}")
+        if timestamps.shape != (pages, page):
+            raise ValueError(f"timestamps must be {(pages, page)}")
+        B, width = page_table.shape
+        if (k_scale is None) != (kind == HSTU_CACHE_BF16) or (v_scale is None) != (k_scale is None):
+            raise ValueError("scales belong to a quantised cache, to both of k and v")
+        if k_scale is not None and (k_scale.shape != (pages, heads, page)
+                                    or v_scale.shape != (pages, heads, page)):
+            raise ValueError(f"scales must be {(pages, heads, page)}")
+        self._arrays = (k, v, timestamps, page_table, lengths, k_scale, v_scale)
+        self._shape = (B, heads, d_qk, d_v)
+        self._desc = CacheDesc(pages, page, width, kind, _array("k", k, k.dtype),
+                               _array("v", v, v.dtype),
+                               _array("k_scale", k_scale, torch.float32),
+                               _array("v_scale", v_scale, torch.float32),
+                               _array("timestamps", timestamps, torch.int64),
+                               _array("page_table", page_table, torch.int32),
+                               _array("lengths", lengths, torch.int64, B))
+
+    k, v, timestamps, page_table, lengths, k_scale, v_scale = (
+        property(lambda self, i=i: self._arrays[i]) for i in range(7))
+
+
+def alloc_cache(num_pages, page_size, num_heads, d_qk, d_v, num_seqs, max_pages,
+                dtype=torch.float8_e4m3fn, device=None) -> PagedCache:
+    """An empty cache: no user owns a page (page_table -1) or a token."""
+    device = device or "cuda"
+
+    def make(dt, *shape):
+        return torch.empty(shape, dtype=dt, device=device)
+    scales = [None if dtype == torch.bfloat16 else
+              make(torch.float32, num_pages, num_heads, page_size) for _ in range(2)]
+    return PagedCache(make(dtype, num_pages, num_heads, page_size, d_qk),
+                      make(dtype, num_pages, num_heads, d_v, page_size),
+                      make(torch.int64, num_pages, page_size),
+                      torch.full((num_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                      torch.zeros(num_seqs, dtype=torch.int64, device=device), *scales)
+
+
+def _cache_batch(cache, seq_offsets):
+    offs, B = _offsets(seq_offsets)
+    if B != cache._shape[0]:
+        raise ValueError(f"{B} sequences, but a cache of {cache._shape[0]}")
+    return offs, B
+
+
+def hstu_cache_write(k, v, timestamps, seq_offsets, cache, starts=None, stream=None):
+    """Writes rows k [T, h, d_qk], v [T, h, d_v] and their timestamps into the
+    cache, token i of sequence b at position starts[b] + i (starts None: i).
+    cache.lengths stays as it is."""
+    offs, B = _cache_batch(cache, seq_offsets)
+    _, H, dqk, dv = cache._shape
+    T = k.shape[0]
+    code = _dtype_code(k)
+    ks = _rows("k", k, (T, H, dqk), k.dtype)
+    vs = _rows("v", v, (T, H, dv), k.dtype)
+    ts = _array("timestamps", timestamps, torch.int64, T)
+    st = _array("starts", starts, torch.int64, B)
+    _on_device(k, v, timestamps, seq_offsets, starts, *cache._arrays)
+    p = Problem(B, T, 1, H, dqk, dv, 1, code)
+    _check(lib.hstu_cache_write(ctypes.byref(p), ctypes.byref(cache._desc), offs, st, ts, _ptr(k),
+                                ks, _ptr(v), vs, _stream(stream)))
+
+
+def hstu_cache_read(cache, seq_offsets, total_tokens, starts=None, dtype=torch.bfloat16, out=None,
+                    stream=None):
+    """(k [T, h, d_qk], v [T, h, d_v], timestamps [T]): row seq_offsets[b] + i is
+    position starts[b] + i of user b (total_tokens = seq_offsets[-1])."""
+    offs, B = _cache_batch(cache, seq_offsets)
+    _, H, dqk, dv = cache._shape
+    T = int(total_tokens)
+    st = _array("starts", starts, torch.int64, B)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    k, v, ts = (None, None, None) if out is None else out
+    k = _dense_out("k", k, cache.k, (T, H, dqk), dtype)
+    v = _dense_out("v", v, cache.k, (T, H, dv), dtype)
+    ts = _dense_out("timestamps", ts, cache.k, (T,), torch.int64)
+    _on_device(seq_offsets, starts, k, v, ts, *cache._arrays)
+    p = Problem(B, T, 1, H, dqk, dv, 1, _dtype_code(k))
+    _check(lib.hstu_cache_read(ctypes.byref(p), ctypes.byref(cache._desc), offs, st, _ptr(k),
+                               _ptr(v), _ptr(ts), _stream(stream)))
+    return k, v, ts
+
+
+def hstu_cache_validate(cache, stream=None):
+    """Raises HstuError where lengths or the page table lead out of the pool."""
+    B, H, dqk, dv = cache._shape
+    _on_device(*cache._arrays)
+    p = Problem(B, 0, 1, H, dqk, dv, 1, HSTU_BF16)
+    _check(lib.hstu_cache_validate(ctypes.byref(p), ctypes.byref(cache._desc), _stream(stream)))
+
+
+# ------------------------------------------------ attention of drafted tokens
+
+HSTU_MAX_DRAFT = 1024
+
+
+def hstu_attn_fwd_tree_workspace_bytes(problem: Problem, cache: PagedCache, max_draft) -> int:
+    return int(lib.hstu_attn_fwd_tree_workspace_bytes(ctypes.byref(problem),
+                                                      ctypes.byref(cache._desc), int(max_draft)))
+
+
+def hstu_attn_fwd_tree(q, k, v, seq_offsets, timestamps, cache, rab_pos, rab_time, max_seq_len,
+                       max_draft, parents=None, out=None, ws=None, stream=None):
+    """O [T, h, d_v] of drafted tokens q, k, v (at most max_draft for each user)
+    over the cached tokens and the nodes on their way to the root (parents [T],
+    None: all are roots); see include/hstu.h."""
+    offs, B = _cache_batch(cache, seq_offsets)
+    _, H, dqk, dv = cache._shape
+    T, dtype = q.shape[0], q.dtype
+    code = _dtype_code(q)
+    qs = _rows("q", q, (T, H, dqk), dtype)
+    ks = _rows("k", k, (T, H, dqk), dtype)
+    vs = _rows("v", v, (T, H, dv), dtype)
+    ts = _array("timestamps", timestamps, torch.int64, T)
+    par = _array("parents", parents, torch.int64, T)
+    rp = _array("rab_pos", rab_pos, torch.float32, 2 * max_seq_len - 1)
+    rt = _array("rab_time", rab_time, torch.float32)
+    out = _dense_out("out", out, q, (T, H, dv), dtype)
+    p = Problem(B, T, max_seq_len, H, dqk, dv, rab_time.numel(), code)
+    if ws is None:
+        n = hstu_attn_fwd_tree_workspace_bytes(p, cache, max_draft)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    _on_device(q, k, v, seq_offsets, timestamps, parents, rab_pos, rab_time, out, ws,
+               *cache._arrays)
+    j = Jagged(offs, ts, None, rp, rt)
+    _check(lib.hstu_attn_fwd_tree(ctypes.byref(p), ctypes.byref(j), ctypes.byref(cache._desc), par,
+                                  int(max_draft), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(out),
+                                  _ptr(ws), ws.numel(), _stream(stream)))
+    return out
+
+
+def hstu_tree_positions(parents, seq_offsets, base, total_tokens, max_draft, out=None,
+                        stream=None):
+    """int64 [T]: base[b] + depth of each drafted token (parents None: depth 0;
+    base None: 0), for hstu_rotary_fwd."""
+    offs, B = _offsets(seq_offsets)
+    T = int(total_tokens)
+    par = _array("parents", parents, torch.int64, T)
+    bs = _array("base", base, torch.int64, B)
+    out = _dense_out("positions", out, seq_offsets, (T,), torch.int64)
+    _on_device(parents, seq_offsets, base, out)
+    _check(lib.hstu_tree_positions(B, T, int(max_draft), offs, par, bs, _ptr(out),
+                                   _stream(stream)))
+    return out
 
 
 def hstu_probe_mfma_bf16(iters: int, waves_per_simd: int, sink: torch.Tensor, stream=None):
