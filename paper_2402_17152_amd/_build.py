@@ -15,7 +15,7 @@ LIB = os.path.join(PKG, "libhstu.so")
 
 SOURCES = ["abi.cpp", "sched.hip", "bucketize.hip", "attn_fwd.hip", "attn_bwd.hip",
            "attn_f32.hip", "ln_gate.hip", "probe.hip", "gemm.hip", "sl.hip", "rotary.hip", "cache.hip",
-           "attn_tree.hip"]
+           "attn_tree.hip", "attn_tree_bf16.hip", "attn_tree_e4m3.hip", "attn_tree_int8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

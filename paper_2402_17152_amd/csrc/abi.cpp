@@ -622,8 +622,25 @@ hstu_status_t check_draft(int32_t max_draft) {
   return HSTU_OK;
 }
 
-// Bytes of workspace; the arguments are checked.
-size_t tree_workspace(const hstu_problem_t*, const hstu_cache_t*, int32_t) { return kAlign; }
+// How the tree attention is cut up and the bytes of workspace it needs for that.
+hstu_status_t tree_plan(const hstu_problem_t* p, const hstu_cache_t* c, int32_t max_draft,
+                        TreeSplit* sp, size_t* bytes) {
+  HSTU_TRY(check_draft(max_draft));
+  const int64_t cap = (int64_t)c->max_pages * c->page_size;
+  if (cap > (int64_t)1 << 30)
+    return fail(HSTU_ERR_UNSUPPORTED, "a page table for more than 2^30 tokens is not supported");
+  *sp = tree_split(p->num_seqs, p->total_tokens, p->num_heads, p->max_seq_len, max_draft, cap);
+  if ((int64_t)p->num_seqs * sp->row_blocks * (sp->chunks + 1) > INT32_MAX ||
+      p->total_tokens > INT32_MAX)
+    return fail(HSTU_ERR_UNSUPPORTED, "%d sequences of %d drafted tokens over %lld cached ones",
+                p->num_seqs, max_draft, (long long)cap);
+  *bytes = kAlign;
+  if (sp->chunks > 1)
+    *bytes = align_up(sizeof(float) * (size_t)(sp->chunks + 1) * (size_t)p->total_tokens *
+                      p->num_heads * p->d_v) +
+             kAlign;
+  return HSTU_OK;
+}
 
 }  // namespace
 
@@ -718,8 +735,12 @@ size_t hstu_attn_fwd_tree_workspace_bytes(const hstu_problem_t* p, const hstu_ca
                                           int32_t max_draft) {
   try {
     CacheArgs a;
-    if (check_cache(p, c, false, &a) != HSTU_OK || check_draft(max_draft) != HSTU_OK) return 0;
-    return tree_workspace(p, c, max_draft);
+    TreeSplit sp;
+    size_t bytes = 0;
+    if (check_cache(p, c, false, &a) != HSTU_OK ||
+        tree_plan(p, c, max_draft, &sp, &bytes) != HSTU_OK)
+      return 0;
+    return bytes;
   } catch (...) {
     return 0;
   }
@@ -738,7 +759,9 @@ hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j
     if (!c->lengths) return fail(HSTU_ERR_INVALID_ARGUMENT, "lengths is NULL");
     if (p->dtype != HSTU_BF16)
       return fail(HSTU_ERR_UNSUPPORTED, "hstu_attn_fwd_tree supports bf16 problems only");
-    HSTU_TRY(check_draft(max_draft));
+    TreeSplit sp;
+    size_t need = 0;
+    HSTU_TRY(tree_plan(p, c, max_draft, &sp, &need));
     const int64_t T = p->total_tokens;
     if (T > (int64_t)p->num_seqs * max_draft)
       return fail(HSTU_ERR_INVALID_ARGUMENT, "%lld drafted tokens are more than %d for each of %d",
@@ -748,7 +771,6 @@ hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j
     HSTU_TRY(check_mat("k", k, k_stride, H * p->d_qk, 2, T));
     HSTU_TRY(check_mat("v", v, v_stride, H * p->d_v, 2, T));
     HSTU_TRY(check_mat("out", out, H * p->d_v, H * p->d_v, 2, T));
-    const size_t need = tree_workspace(p, c, max_draft);
     if (!ws) return fail(HSTU_ERR_WORKSPACE, "workspace is NULL (need %zu bytes)", need);
     if ((uintptr_t)ws % kAlign)
       return fail(HSTU_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -763,8 +785,9 @@ hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j
     a.d_qk = p->d_qk;
     a.d_v = p->d_v;
     a.out = out;
+    sp.part = sp.chunks > 1 ? (float*)ws : nullptr;
     TimedScope ts("attn_fwd_tree", s);
-    HSTU_HIP(launch_attn_tree(a, cache_kind(c), s), "attn_fwd_tree launch");
+    HSTU_HIP(launch_attn_tree(a, sp, cache_kind(c), s), "attn_fwd_tree launch");
     return ok();
   } catch (...) {
     return fail(HSTU_ERR_INVALID_ARGUMENT, "internal error");
