@@ -436,8 +436,9 @@ hstu_status_t hstu_rotary_bwd(const hstu_problem_t* p, const int64_t* seq_offset
  *   timestamps        int64 [num_pages][page_size]
  * A row is one token of one head; what is held of a row x is
  *   BF16    x rounded to bf16;
- *   INT8    code * s, s = max|x| / 127 rounded to fp32, code = x / s rounded
- *           to the nearest integer (ties to even);
+ *   INT8    code * s, s = max|x| * r rounded to fp32 with r the fp32 number
+ *           nearest to 1/127, code = x / s rounded to the nearest integer
+ *           (ties to even);
  *   E4M3    code * s, s the smallest power of two (at most 2^119) with
  *           max|x| <= 448 s, code = x / s rounded to the nearest 8-bit float of
  *           4 exponent and 3 mantissa bits (no infinities, largest 448; ties

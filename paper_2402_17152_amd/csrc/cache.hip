@@ -78,7 +78,7 @@ __device__ __forceinline__ uint2 quantise(const float* x, uint32_t top, float* s
   }
   uint32_t w[2];
   if constexpr (KIND == kCacheInt8) {
-    const float s = __fdiv_rn(big, 127.0f);
+    const float s = big * (1.0f / 127.0f);
     const float inv = 1.0f / s;
 #pragma unroll
     for (int i = 0; i < 2; i++) {

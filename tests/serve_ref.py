@@ -42,7 +42,7 @@ def quantise(x, kind):
         if top < 2.0 ** -100:
             continue
         if kind == "int8":
-            s = float(np.float32(top / 127.0))
+            s = float(np.float32(top * float(np.float32(1.0 / 127.0))))
             codes[at] = np.rint(row / s)
         else:
             e = -200

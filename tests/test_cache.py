@@ -125,6 +125,7 @@ def test_reference_quantiser():
     c, s = ref.quantise([[449.0, 1.0, 0.0], [127.0, 63.5, -62.5]], "e4m3")
     assert s[0] == 2.0 and c[0].tolist() == [224.0, 0.5, 0.0]
     c, s = ref.quantise([[127.0, 63.5, -62.5], [0.0, 0.0, 0.0], [1.0, np.inf, 2.0]], "int8")
+    # 127 times the fp32 number nearest to 1/127, which is below it, rounds to 1
     assert c[0].tolist() == [127.0, 64.0, -62.0] and s[0] == 1.0
     assert s[1] == 1.0 and np.isnan(s[2]) and not c[2].any()
     assert len(ref.e4m3_values()) == 127 and ref.e4m3_values()[-1] == 448.0
