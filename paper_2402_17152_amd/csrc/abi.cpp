@@ -630,15 +630,13 @@ hstu_status_t tree_plan(const hstu_problem_t* p, const hstu_cache_t* c, int32_t 
   if (cap > (int64_t)1 << 30)
     return fail(HSTU_ERR_UNSUPPORTED, "a page table for more than 2^30 tokens is not supported");
   *sp = tree_split(p->num_seqs, p->total_tokens, p->num_heads, p->max_seq_len, max_draft, cap);
-  if ((int64_t)p->num_seqs * sp->row_blocks * (sp->chunks + 1) > INT32_MAX ||
-      p->total_tokens > INT32_MAX)
+  if ((int64_t)p->num_seqs * sp->row_blocks * sp->chunks * p->num_heads > INT32_MAX ||
+      (int64_t)p->num_seqs * max_draft > INT32_MAX)
     return fail(HSTU_ERR_UNSUPPORTED, "%d sequences of %d drafted tokens over %lld cached ones",
                 p->num_seqs, max_draft, (long long)cap);
-  *bytes = kAlign;
-  if (sp->chunks > 1)
-    *bytes = align_up(sizeof(float) * (size_t)(sp->chunks + 1) * (size_t)p->total_tokens *
-                      p->num_heads * p->d_v) +
-             kAlign;
+  *bytes = align_up(sizeof(float) * (size_t)sp->chunks * (size_t)p->total_tokens * p->num_heads *
+                    p->d_v) +
+           kAlign;
   return HSTU_OK;
 }
 
@@ -785,7 +783,7 @@ hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j
     a.d_qk = p->d_qk;
     a.d_v = p->d_v;
     a.out = out;
-    sp.part = sp.chunks > 1 ? (float*)ws : nullptr;
+    sp.part = (float*)ws;
     TimedScope ts("attn_fwd_tree", s);
     HSTU_HIP(launch_attn_tree(a, sp, cache_kind(c), s), "attn_fwd_tree launch");
     return ok();

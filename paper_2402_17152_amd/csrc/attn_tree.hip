@@ -10,38 +10,162 @@ namespace {
 
 using tree::kThreads;
 
-// out = (sum over a user's chunks, in order, and the drafted part) / N.  A wave
-// takes 64 groups of 4 features of a row, four waves a quarter of the chunks each.
-__global__ __launch_bounds__(kThreads) void tree_join_kernel(const TreeArgs a, const TreeSplit sp) {
-  __shared__ f32x4 sums[3][64];
-  const int64_t t = blockIdx.x;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int b = find_seq(a.ja.seq_offsets, a.ja.num_seqs, t);
+constexpr int kLevels = 10;  // ways of up to 2^10 nodes
+
+// Places in a forest: up[l][i] is the node 2^l steps above node i, or -1.
+struct Ways {
+  short up[kLevels][kMaxDraft];
+};
+
+// Fills the ways of the nodes below n; returns the number of levels in use (the
+// same for all threads).  Ends past a barrier.
+__device__ __forceinline__ int climb(const int64_t* parents, int n, Ways* w) {
+  bool more = false;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int64_t p = parents[i];
+    const short x = p >= 0 && p < i ? (short)p : (short)-1;
+    w->up[0][i] = x;
+    more |= x >= 0;
+  }
+  int l = 0;
+  while (__syncthreads_or(more) && ++l < kLevels) {
+    more = false;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const short x = w->up[l - 1][i];
+      const short y = x >= 0 ? w->up[l - 1][x] : (short)-1;
+      w->up[l][i] = y;
+      more |= y >= 0;
+    }
+  }
+  return l;
+}
+
+__device__ __forceinline__ void add8(float* x, u32x4 v, float w) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    x[2 * i] = fmaf(w, __uint_as_float(v[i] << 16), x[2 * i]);
+    x[2 * i + 1] = fmaf(w, __uint_as_float(v[i] & 0xffff0000u), x[2 * i + 1]);
+  }
+}
+
+// The drafted keys of a row and head (the row's own and those on its way to the
+// root), added to the partial outputs of the cached ones, in order; out = the sum
+// / N.  A wave takes a row and head: d / 8 lanes share a key or a partial output,
+// so several of them are under way at once.  Latency-bound for few rows, then
+// bound by the partial outputs' bytes.  Where there are many chunks the four waves
+// of a workgroup share a row and head (`waves` 4).
+template <int DQK, int DV>
+__global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
+                                                               const TreeSplit sp, int per,
+                                                               int waves) {
+  constexpr int LK = DQK / 8, LV = DV / 8;  // lanes of a K row, of a V row
+  __shared__ Ways ways;
+  __shared__ float weight[kThreads / 64][64];
+  __shared__ float rest[kThreads / 64 - 1][DV];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int H = a.ja.num_heads;
+  const int blocks = (a.max_draft + per - 1) / per;
+  const int b = blockIdx.x / blocks, r0 = blockIdx.x % blocks * per;
   const int64_t o = a.ja.seq_offsets[b];
-  if (t < o || t - o >= a.max_draft || t >= a.ja.seq_offsets[b + 1]) return;
+  const int64_t o1 = min(a.ja.seq_offsets[b + 1], a.ja.total_tokens);
+  const int L = (int)max((int64_t)0, min(o1 - o, (int64_t)a.max_draft));
+  if (o < 0 || r0 >= L) return;
   const int64_t cap = (int64_t)a.c.max_pages << a.c.lg_page;
   const int64_t n_b = max((int64_t)0, min(a.c.lengths[b], cap));
   const int used = (int)((n_b + sp.chunk_len - 1) / sp.chunk_len);
-  const int width = a.ja.num_heads * a.d_v / 4, c = blockIdx.y * 64 + lane;
-  const int64_t slot = a.ja.total_tokens * width;
-  const f32x4* src = reinterpret_cast<const f32x4*>(sp.part) + t * width + c;
-  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (c < width) {
-    const int per = (used + 3) / 4;
-    const int end = min(used, (wave + 1) * per);
-#pragma unroll 8
-    for (int i = wave * per; i < end; i++) sum += src[i * slot];
-    if (wave == 3) sum += src[sp.chunks * slot];
+  const int rows = min(per, L - r0);
+  const int levels = a.parents ? climb(a.parents + o, r0 + rows, &ways) : 0;
+  const int N = a.ja.max_seq_len;
+  const int share = waves == 1 ? 0 : wave;  // of the chunks
+  const int pairs = rows * (waves == 1 ? H : 1);
+  for (int pair = waves == 1 ? wave : 0; pair < pairs; pair += waves == 1 ? kThreads / 64 : 1) {
+    const int i = r0 + (waves == 1 ? pair / H : pair);
+    const int head = waves == 1 ? pair % H : blockIdx.y;
+    const int64_t t = o + i;
+    float x[8] = {};
+    {
+      const int64_t slot = a.ja.total_tokens * H * DV;
+      const float* src = sp.part + (t * H + head) * DV + 8 * (lane % LV);
+      const int step = 64 / LV * waves;
+#pragma unroll 4
+      for (int c = share * (64 / LV) + lane / LV; c < used; c += step) {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(src + c * slot);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(src + c * slot + 4);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          x[e] += lo[e];
+          x[4 + e] += hi[e];
+        }
+      }
+      // the weights' factor -log2(e) comes off
+#pragma unroll
+      for (int e = 0; e < 8; e++) x[e] *= -0.6931471805599453f;
+    }
+    if (share == 0) {
+      int count = 1;  // nodes on the way, this one included
+      for (int l = levels - 1, n = i; l >= 0; l--)
+        if (ways.up[l][n] >= 0) {
+          count += 1 << l;
+          n = ways.up[l][n];
+        }
+      auto above = [&](int steps) {
+        int n = i;
+        for (int l = 0; l < levels; l++)
+          if ((steps >> l) & 1) n = ways.up[l][n];
+        return n;
+      };
+      float q[8] = {};
+      add8(q, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.q + t * a.t.q_stride +
+                                              head * DQK + 8 * (lane % LK)), 1.0f);
+      const int64_t time = a.ja.timestamps[t];
+      for (int w0 = 0; w0 < count; w0 += 64) {
+        const int here = min(64, count - w0);
+        for (int y = lane / LK; y < here; y += 64 / LK) {
+          const int64_t n = o + above(w0 + y);
+          float k[8] = {};
+          add8(k, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.k + n * a.t.k_stride +
+                                                  head * DQK + 8 * (lane % LK)), 1.0f);
+          float s = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; e++) s = fmaf(q[e], k[e], s);
+#pragma unroll
+          for (int m = 1; m < LK; m *= 2) s += __shfl_xor(s, m, 64);
+          s += a.ja.rab_pos[max(0, N - 1 - (w0 + y))] +
+               a.ja.rab_time[time_bucket64(time - a.ja.timestamps[n], a.ja.num_buckets)];
+          if (lane % LK == 0) weight[wave][y] = s * sigmoid_fast(s);
+        }
+        __builtin_amdgcn_wave_barrier();
+        for (int y = lane / LV; y < here; y += 64 / LV)
+          add8(x, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.v +
+                                                  (o + above(w0 + y)) * a.t.v_stride +
+                                                  head * DV + 8 * (lane % LV)), weight[wave][y]);
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+#pragma unroll
+    for (int m = LV; m < 64; m *= 2)
+#pragma unroll
+      for (int e = 0; e < 8; e++) x[e] += __shfl_xor(x[e], m, 64);
+    if (waves > 1) {
+      if (share > 0 && lane < LV)
+#pragma unroll
+        for (int e = 0; e < 8; e++) rest[share - 1][8 * lane + e] = x[e];
+      __syncthreads();
+      if (share == 0)
+#pragma unroll
+        for (int w = 0; w < kThreads / 64 - 1; w++)
+#pragma unroll
+          for (int e = 0; e < 8; e++) x[e] += rest[w][8 * (lane % LV) + e];
+      __syncthreads();
+      if (share > 0) continue;
+    }
+    if (lane < LV) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) x[e] /= (float)N;
+      *reinterpret_cast<u32x4*>((uint16_t*)a.out + (t * H + head) * DV + 8 * lane) =
+          pack_bf16x8(x);
+    }
   }
-  if (wave) sums[wave - 1][lane] = sum;
-  __syncthreads();
-  if (wave || c >= width) return;
-  sum = ((sum + sums[0][lane]) + sums[1][lane]) + sums[2][lane];
-  sum *= 1.0f / (float)a.ja.max_seq_len;
-  uint2 w;
-  w.x = pack_bf16x2(sum[0], sum[1]);
-  w.y = pack_bf16x2(sum[2], sum[3]);
-  reinterpret_cast<uint2*>(a.out)[t * width + c] = w;
 }
 
 // positions = base + depth of every drafted token.
@@ -55,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void tree_positions_kernel(int64_t total,
   const int64_t o = offs[b];
   if (o < 0) return;
   const int n = (int)max((int64_t)0, min(min(offs[b + 1], total) - o, (int64_t)max_draft));
-  tree::walk<false>(parents ? parents + o : nullptr, n, 0, node, nullptr);
+  tree::walk(parents ? parents + o : nullptr, n, node);
   const int64_t p0 = base ? base[b] : 0;
   for (int i = threadIdx.x; i < n; i += kThreads) positions[o + i] = p0 + node[i].y;
 }
@@ -64,18 +188,20 @@ __global__ __launch_bounds__(kThreads) void tree_positions_kernel(int64_t total,
 
 TreeSplit tree_split(int32_t num_seqs, int64_t total_tokens, int32_t num_heads, int32_t max_seq_len,
                      int32_t max_draft, int64_t cap) {
-  constexpr int64_t kWanted = 768;  // workgroups
+  constexpr int64_t kWanted = 512;  // workgroups: two for each compute unit
   TreeSplit sp{};
-  sp.rows = max_draft <= 16 ? 16 : 32;
+  sp.rows = max_draft <= 16 ? 16 : max_draft <= 32 ? 32 : max_draft <= 64 ? 64 : 128;
   sp.row_blocks = (max_draft + sp.rows - 1) / sp.rows;
   const int64_t blocks =
       std::min((int64_t)num_seqs * sp.row_blocks, total_tokens / sp.rows + num_seqs);
   const int64_t keys = std::min(cap, (int64_t)max_seq_len);
   const int64_t most = (keys + tree::kBlock - 1) / tree::kBlock;
-  sp.hg = num_heads % 4 == 0 ? 4 : num_heads % 2 == 0 ? 2 : 1;
+  // Four waves: heads, rows in 32s, then shares of the keys.
+  sp.hg = sp.rows > 64 ? 1 : sp.rows > 32 ? 2 : 4;
+  while (num_heads % sp.hg) sp.hg /= 2;
   while (sp.hg > 1 && blocks * (num_heads / sp.hg) * most < kWanted) sp.hg /= 2;
   const int64_t base = blocks * (num_heads / sp.hg);
-  const int64_t chunks = std::max((int64_t)1, std::min(most, (kWanted + base - 1) / base));
+  const int64_t chunks = std::max((int64_t)1, std::min(most, (kWanted + base / 2) / base));
   sp.chunk_len = (int32_t)((most + chunks - 1) / chunks * tree::kBlock);
   sp.chunks = (int32_t)((cap + sp.chunk_len - 1) / sp.chunk_len);
   return sp;
@@ -85,11 +211,23 @@ hipError_t launch_attn_tree(const TreeArgs& a, const TreeSplit& sp, int kind, hi
   hipError_t e = kind == kCacheBf16   ? tree::launch_bf16(a, sp, s)
                  : kind == kCacheE4m3 ? tree::launch_e4m3(a, sp, s)
                                       : tree::launch_int8(a, sp, s);
-  if (e != hipSuccess || !sp.part) return e;
-  const dim3 grid((unsigned)a.ja.total_tokens,
-                  (unsigned)((a.ja.num_heads * a.d_v / 4 + 63) / 64));
-  hipLaunchKernelGGL(tree_join_kernel, grid, dim3(kThreads), 0, s, a, sp);
-  return hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int waves = sp.chunks > 16 ? 4 : 1;
+  const int per = waves == 4 ? 1 : std::min(4, a.max_draft);
+  const dim3 grid((unsigned)((int64_t)a.ja.num_seqs * ((a.max_draft + per - 1) / per)),
+                  waves == 4 ? (unsigned)a.ja.num_heads : 1u);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, sp, per, waves);
+    return hipGetLastError();
+  };
+#define HSTU_FINISH_DV(DQK)                                    \
+  return a.d_v == 32   ? go(tree_finish_kernel<DQK, 32>)       \
+         : a.d_v == 64 ? go(tree_finish_kernel<DQK, 64>)       \
+                       : go(tree_finish_kernel<DQK, 128>);
+  if (a.d_qk == 32) { HSTU_FINISH_DV(32) }
+  if (a.d_qk == 64) { HSTU_FINISH_DV(64) }
+  HSTU_FINISH_DV(128)
+#undef HSTU_FINISH_DV
 }
 
 hipError_t launch_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_t max_draft,

@@ -330,14 +330,14 @@ struct TreeArgs {
 };
 // How a call is cut up.
 struct TreeSplit {
-  float* part;        // partial outputs [chunks + 1][T][h][d_v], or null: out is final
-  int32_t chunks;     // items of cached keys for each user; one more takes the drafted ones
+  float* part;        // partial outputs [chunks][T][h][d_v] of the cached keys
+  int32_t chunks;     // for each user
   int32_t chunk_len;  // keys of a chunk
   int32_t hg;         // heads a workgroup takes: 1, 2 or 4
   int32_t rows;       // drafted rows it takes
   int32_t row_blocks;
 };
-// The split for these sizes; part is left null, and stays so if chunks is 1.
+// The split for these sizes, part left null.
 TreeSplit tree_split(int32_t num_seqs, int64_t total_tokens, int32_t num_heads, int32_t max_seq_len,
                      int32_t max_draft, int64_t cap);
 hipError_t launch_attn_tree(const TreeArgs& a, const TreeSplit& sp, int kind, hipStream_t s);
