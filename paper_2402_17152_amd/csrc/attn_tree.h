@@ -1,21 +1,19 @@
-// Attention of drafted tokens over the paged cache (include/hstu.h): the kernel of
+// Attention of drafted tokens over the paged cache (include/hstu.h): the kernels of
 // the cached keys, instantiated for one kind of cache in each of
 // attn_tree_{bf16,e4m3,int8}.hip.  Weights are pointwise, so sums over parts of the
-// keys simply add up: the kernel leaves fp32 partial outputs, and a second one
+// keys simply add up: the kernels leave fp32 partial outputs, and another one
 // (attn_tree.hip) adds them to the drafted keys' part.
 //
-// A workgroup of four waves takes some drafted rows of one user, a chunk of the
-// cached keys and `hg` heads; a wave takes one head, 16 R of the rows and every
-// ks_count-th tile of T keys.  Waves of other rows of the same head load the same
-// cached rows at the same time, which then come from the vector cache.
+// A workgroup of four waves takes some drafted rows of one user and a chunk of the
+// cached keys, in tiles of T keys.
 //
 //   S^T = K Q^T on 16x16x32 matrix instructions, keys in the rows: lane
 //   (row r = l % 16, group g = l / 16) of K's operand t reads key T/4 (r/4) + 4t +
 //   r%4, so that accumulator t leaves keys T/4 g + 4 t + 0..3 of query row l % 16
 //   in lane l.  That is the layout of the weights as the left operand of O = P V,
 //   whose contraction runs over keys T/4 g + 8 s + 0..7: no exchange between lanes.
-//   The cache holds V transposed, so its operand (T/4 keys of a feature) is one
-//   load.  Nothing passes through LDS but what all heads and rows share.
+//   The cache holds V transposed, so its operand (T/4 keys of a feature) is 16 bytes
+//   in a row.
 //
 // Codes of 8 bits are exact in bf16; a key's scales multiply the score and the
 // weight.  Everything is kept times -log2(e): y = -log2(e) s gives SiLU(s) =
@@ -24,7 +22,19 @@
 // scales, the times and the window of rab_pos that its rows can reach; where the
 // time bucket of a row is the same for all keys of a tile (most of a long history:
 // buckets are powers of two) the time bias is one number.
+//
+// Up to 32 rows, attn_tree_few_kernel: what counts is how fast the cache streams in.
+// A wave takes a head (and a share of the keys) and loads the operands straight into
+// registers, a tile ahead.  Lanes that are neighbours read different rows then, 16
+// bytes each, and the vector cache takes one such access a clock: 9.8 TB/s, above
+// the memory's rate but not by enough to load anything twice.
+// More rows, attn_tree_many_kernel: the four waves take 16 R rows each of one head
+// and share its tiles through LDS, loaded in rows of 64 bytes and more (a fourth of
+// the accesses; loaded by each wave for itself, 16 x 1024 rows over 1024-2048 keys
+// spent 183 of 230 us on them).
 #pragma once
+
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -37,20 +47,26 @@ constexpr int kWindow = 512;      // entries of rab_pos that are held
 constexpr int kMaxRows = 128;     // drafted rows of a workgroup
 constexpr float kNegLog2e = -kLog2e;
 
-// What is known of the times of a tile's keys against a row's.
-enum { kTimesAny = 0, kTimesNear = 1, kTimesOne = 2 };
+// What is known of 64 keys: each row's time bucket is the same for all; the time
+// differences fit 32 bits; all of the first, the second 32 keys are there.
+enum { kOneBucket = 1, kNear = 2, kWhole = 4 };
 
-// What the waves of a workgroup share.
-struct Shared {
-  float scales[2][4][kBlock];      // of the block's keys, k (times -log2(e)) and v, per head
+// What the waves of a workgroup know of kBlock keys; HG: heads.
+template <int HG>
+struct Keys {
+  float scales[2][HG][kBlock];     // k (times -log2(e)) and v
   float window[4][kWindow + 8];    // part of rab_pos (times -log2(e)), four shifted copies
-  int64_t time[kBlock];            // of the keys
-  int64_t rows16[kBlock / 16];     // first cache row of 16 keys for head 0, or -1
-  short2 node[kMaxDraft];          // depths (y) of the drafted tokens
+  int64_t time[kBlock];
+  int64_t rows16[kBlock / 16];     // first cache row of 16 keys for head 0
+  int left16[kBlock / 16];         // how many of them are there; of none, row 0 is read
+  float uniform[4][kMaxRows];      // the rows' entry of rtime for 64 keys (kOneBucket)
+  int about[4];                    // what is known of 64 keys
+};
+
+// What they know of the drafted rows.
+struct Rows {
   float rtime[256];                // rab_time, times -log2(e)
-  int64_t row_time[kMaxRows];
-  float uniform[4][kMaxRows];      // the rows' entry of rtime for 64 keys (kTimesOne)
-  int times[4];                    // kTimes* of 64 keys
+  int64_t time[kMaxRows];
 };
 
 // Two words of codes (8 of them) as bf16.
@@ -159,9 +175,292 @@ __device__ __forceinline__ int64_t wave_extreme64(int64_t v) {
   return (int64_t)top << 32 | (uint32_t)(lo ^ (int)0x80000000u);
 }
 
+// A workgroup's part of the work.
+struct Part {
+  int b, head0, hg;        // user, first head, heads
+  int from, to;            // cached keys
+  int64_t o;               // first drafted token of the user
+  int r0, rows;            // drafted rows: r0 .. r0 + rows - 1 of the user's
+  int n_b, cap, lg;        // cached tokens, room for them, log2 of the page size
+  int deep, flat;          // depths of the rows: the largest, the smallest
+  bool windowed;           // Keys::window holds all that the rows reach
+};
+
+// The user, rows and keys of a workgroup; false: there is nothing to do.
+__device__ __forceinline__ bool find_part(const TreeArgs& a, const TreeSplit& sp, Part* w) {
+  // Workgroups go to the eight dies in turn: the row blocks of one chunk and
+  // head group, which read the same keys, follow each other on one die.
+  const int die = blockIdx.x % 8, turn = blockIdx.x / 8;
+  const int rb = turn % sp.row_blocks;
+  const int unit = turn / sp.row_blocks * 8 + die;
+  const int hgs = a.ja.num_heads / sp.hg;
+  const int item = unit / hgs % sp.chunks;
+  w->b = unit / hgs / sp.chunks;
+  if (w->b >= a.ja.num_seqs) return false;
+  w->hg = sp.hg;
+  w->head0 = unit % hgs * sp.hg;
+  w->lg = a.c.lg_page;
+  w->cap = a.c.max_pages << w->lg;
+  w->from = item * sp.chunk_len;
+  w->o = a.ja.seq_offsets[w->b];
+  const int64_t o1 = min(a.ja.seq_offsets[w->b + 1], a.ja.total_tokens);
+  w->n_b = (int)max((int64_t)0, min(a.c.lengths[w->b], (int64_t)w->cap));
+  const int L = (int)max((int64_t)0, min(o1 - w->o, (int64_t)a.max_draft));
+  w->r0 = rb * sp.rows;
+  w->to = min(w->n_b, w->from + sp.chunk_len);
+  w->rows = min(sp.rows, L - w->r0);
+  return w->o >= 0 && w->r0 < L && w->from < w->to;
+}
+
+// What a thread knows of key k0 + its number, before it is in LDS.
+template <int HG>
+struct Ahead {
+  int64_t page, time;
+  float ks[HG], vs[HG], pos[kWindow / kThreads];
+};
+
+__device__ __forceinline__ int fetch_page(const TreeArgs& a, const Part& w, int k0) {
+  const int j = k0 + (int)threadIdx.x;
+  return j < w.cap ? a.c.page_table[(int64_t)w.b * a.c.max_pages + (j >> w.lg)] : -1;
+}
+
+template <bool Q8, int HG>
+__device__ __forceinline__ void fetch(const TreeArgs& a, const Part& w, int k0, int page,
+                                      Ahead<HG>* h) {
+  const int j = k0 + (int)threadIdx.x, place = j & ((1 << w.lg) - 1);
+  h->page = j < w.to && page < a.c.num_pages ? page : -1;
+  h->time = h->page >= 0 ? a.c.tc[(h->page << w.lg) + place] : 0;
+  if constexpr (Q8)
+#pragma unroll
+    for (int x = 0; x < HG; x++) {
+      const int64_t at = ((h->page * a.ja.num_heads + w.head0 + x) << w.lg) + place;
+      const bool on = h->page >= 0 && x < w.hg;
+      h->ks[x] = on ? a.c.k_scale[at] : 0.0f;
+      h->vs[x] = on ? a.c.v_scale[at] : 0.0f;
+    }
+}
+
+// The part of rab_pos that the pairs of a block can reach: entry x belongs to
+// x = key - k0 + deep - depth.
+template <int HG>
+__device__ __forceinline__ void fetch_pos(const TreeArgs& a, const Part& w, int k0, Ahead<HG>* h) {
+  const int N = a.ja.max_seq_len, base = N - 1 + k0 - w.n_b - w.deep + (int)threadIdx.x;
+  if (w.windowed)
+#pragma unroll
+    for (int e = 0; e < kWindow / kThreads; e++)
+      h->pos[e] = a.ja.rab_pos[max(0, min(2 * N - 2, base + e * kThreads))];
+}
+
+// Where the rows of a block's keys are.
+template <int HG>
+__device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k0,
+                                         const Ahead<HG>& h, Keys<HG>* k) {
+  const uint64_t there = __ballot(h.page >= 0);
+  const int tid = threadIdx.x;
+  if (tid % 16 == 0) {
+    // keys of 16 lie on one page, the last ones may be missing
+    k->rows16[tid / 16] =
+        h.page >= 0 ? ((h.page * a.ja.num_heads) << w.lg) + ((k0 + tid) & ((1 << w.lg) - 1)) : 0;
+    k->left16[tid / 16] = __popc((uint32_t)(there >> (tid % 64)) & 0xffffu);
+  }
+}
+
+// The rest of what is known of them.
+template <bool Q8, int HG>
+__device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const Rows& rows,
+                                         const Ahead<HG>& h, Keys<HG>* k) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  k->time[tid] = h.time;
+  if constexpr (Q8)
+#pragma unroll
+    for (int x = 0; x < HG; x++)
+      if (x < w.hg) {
+        k->scales[0][x][tid] = h.ks[x] * kNegLog2e;
+        k->scales[1][x][tid] = h.vs[x];
+      }
+  // Copy c of the window starts c entries later: any four in a row are one
+  // aligned read of some copy.
+  if (w.windowed)
+#pragma unroll
+    for (int e = 0; e < kWindow / kThreads; e++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        const int x = tid + e * kThreads - c;
+        if (x >= 0) k->window[c][x] = h.pos[e] * kNegLog2e;
+      }
+  // What the rows' times have in common with those of this wave's 64 keys:
+  // |dt| is monotone in the key's time on either side of 0.
+  const bool ok = h.page >= 0;
+  const uint64_t there = __ballot(ok);
+  const int64_t lo = wave_extreme64<false>(ok ? h.time : INT64_MAX);
+  const int64_t hi = wave_extreme64<true>(ok ? h.time : INT64_MIN);
+  bool one = true, near = true;
+  for (int i = lane; lo <= hi && i < w.rows; i += 64) {
+    const int64_t x = rows.time[i] - lo, y = rows.time[i] - hi;
+    const int bx = time_bucket64(x, a.ja.num_buckets);
+    const int by = time_bucket64(y, a.ja.num_buckets);
+    one &= bx == by && ((x >= 0) == (y >= 0) || bx == 0);
+    near &= x == (int)x && y == (int)y && (int)x != INT32_MIN && (int)y != INT32_MIN;
+    k->uniform[wave][i] = rows.rtime[by];
+  }
+  const int all_one = __ballot(!one) == 0 ? kOneBucket : 0;
+  const int all_near = __ballot(!near) == 0 ? kNear : 0;
+  const int whole =
+      ((uint32_t)there == ~0u ? kWhole : 0) | (there >> 32 == 0xffffffffu ? 2 * kWhole : 0);
+  if (lane == 0) k->about[wave] = all_one | all_near | whole;
+}
+
+// Depths of this lane's rows w0 + 16 m + r (0 where there is none), and the extremes
+// of all rows.  Ends past a barrier if `node` is used.
+template <int R>
+__device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, short2* node,
+                                            int* depth) {
+  const int lane = threadIdx.x % 64, r = lane % 16;
+  const int64_t* parents = a.parents ? a.parents + w->o : nullptr;
+  const int nodes = w->r0 + w->rows;
+  w->deep = w->flat = 0;
+#pragma unroll
+  for (int m = 0; m < R; m++) depth[m] = 0;
+  if (parents) {
+    int deep = 0, flat = kMaxDraft;
+    if (nodes <= 64) {
+      const int64_t p = lane < nodes ? parents[lane] : -1;
+      const int d = walk64(p >= 0 && p < lane ? (int)p : -1);
+#pragma unroll
+      for (int m = 0; m < R; m++) {
+        const int x = __shfl(d, (w->r0 + w0 + 16 * m + r) & 63, 64);
+        if (w0 + 16 * m + r < w->rows) depth[m] = x;
+      }
+      if (lane >= w->r0 && lane < nodes) deep = flat = d;
+    } else {
+      walk(parents, nodes, node);
+      for (int i = w->r0 + lane; i < nodes; i += 64) {
+        deep = max(deep, (int)node[i].y);
+        flat = min(flat, (int)node[i].y);
+      }
+#pragma unroll
+      for (int m = 0; m < R; m++)
+        if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
+    }
+    w->deep = wave_extreme<true>(deep);
+    w->flat = wave_extreme<false>(flat);
+  }
+  w->windowed = w->deep - w->flat < kWindow - kBlock;
+}
+
+// Q as the right operand: rows w0 + 16 m + r, features in the order of feature().
+template <int KIND, int DQK, int R>
+__device__ __forceinline__ void load_q(const TreeArgs& a, const Part& w, int w0, int head,
+                                       bf16x8 (&q)[R][DQK / 32]) {
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+#pragma unroll
+  for (int m = 0; m < R; m++) {
+    const int row = w0 + 16 * m + r;
+    const uint16_t* src =
+        (const uint16_t*)a.t.q + (w.o + w.r0 + row) * a.t.q_stride + (int64_t)head * DQK;
+#pragma unroll
+    for (int s = 0; s < DQK / 32; s++) {
+      u32x4 v = zero_u32x4();
+      if (row < w.rows) v = *reinterpret_cast<const u32x4*>(src + feature<KIND, DQK>(s, g));
+      q[m][s] = as_bf16x8(v);
+    }
+  }
+}
+
+// -log2(e) times the bias of this lane's rows and the eight keys k0 + at ..
+template <int HG, int R>
+__device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, const Rows& rows,
+                                          const Keys<HG>& k, int about, int k0, int at, int w0,
+                                          const int* depth, f32x4 (&bv)[R][2]) {
+  const int r = threadIdx.x % 16;
+  if (w.windowed && (about & kOneBucket)) {
+#pragma unroll
+    for (int m = 0; m < R; m++) {
+      const float one = k.uniform[at / 64][w0 + 16 * m + r];
+      const int shift = max(0, min(w.deep - depth[m], kWindow - kBlock - 1));
+      const float* win = &k.window[shift & 3][(shift & ~3) + at];
+#pragma unroll
+      for (int x = 0; x < 2; x++) bv[m][x] = *reinterpret_cast<const f32x4*>(win + 4 * x) + one;
+    }
+    return;
+  }
+  const int N = a.ja.max_seq_len;
+#pragma unroll
+  for (int m = 0; m < R; m++) {
+    const int64_t rt = rows.time[w0 + 16 * m + r];
+    const int shift = max(0, min(w.deep - depth[m], kWindow - kBlock - 1));
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int far = N - 1 + k0 + at + i - w.n_b - depth[m];
+      const float pos =
+          w.windowed ? k.window[0][shift + at + i] : a.ja.rab_pos[max(0, far)] * kNegLog2e;
+      const int64_t kt = k.time[at + i];
+      int bucket;
+      if (about & kNear) {
+        const int dt = (int)rt - (int)kt;
+        bucket = min(31 - __clz(max(1, max(dt, -dt))), a.ja.num_buckets - 1);
+      } else {
+        bucket = time_bucket64(rt - kt, a.ja.num_buckets);
+      }
+      bv[m][i / 4][i % 4] = pos + rows.rtime[bucket];
+    }
+  }
+}
+
+// The weights (times -log2(e)) of a row and eight keys as the left operand of P V:
+// scores sc, their bias, the keys' scales; keys from `left` on count nothing.
+template <bool Q8>
+__device__ __forceinline__ bf16x8 find_weights(const f32x4* sc, const f32x4* bv, const f32x4* kf,
+                                               const f32x4* vf, bool whole, int left) {
+  float w[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    float y;
+    if constexpr (Q8) y = fmaf(sc[i / 4][i % 4], kf[i / 4][i % 4], bv[i / 4][i % 4]);
+    else y = fmaf(sc[i / 4][i % 4], kNegLog2e, bv[i / 4][i % 4]);
+    y *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
+    if constexpr (Q8) y *= vf[i / 4][i % 4];
+    w[i] = y;
+  }
+  if (!whole)
+#pragma unroll
+    for (int i = 0; i < 8; i++) w[i] = i < left ? w[i] : 0.0f;
+  return as_bf16x8(pack_bf16x8(w));
+}
+
+// 16 bytes of codes with those behind the first `left` zeroed.
+template <int CB>
+__device__ __forceinline__ u32x4 cut(u32x4 v, int left) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const int keep = (left * CB - 4 * e) * 8;  // bits
+    v[e] = keep >= 32 ? v[e] : keep <= 0 ? 0u : v[e] & ((1u << keep) - 1u);
+  }
+  return v;
+}
+
+// Partial outputs of a wave's rows and head.
+template <int DV, int R>
+__device__ __forceinline__ void put_part(const TreeArgs& a, const TreeSplit& sp, const Part& w,
+                                         int w0, int head, const f32x4 (&acc)[R][DV / 16]) {
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+  const int64_t item = w.from / sp.chunk_len;
+#pragma unroll
+  for (int m = 0; m < R; m++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int row = w0 + 16 * m + 4 * g + i;
+      if (row >= w.rows) continue;
+      float* dst = sp.part + ((item * a.ja.total_tokens + w.o + w.r0 + row) * a.ja.num_heads +
+                              head) * DV + r;
+#pragma unroll
+      for (int c = 0; c < DV / 16; c++) dst[16 * c] = acc[m][c][i];
+    }
+}
+
 template <int KIND, int DQK, int DV, int R>
-__global__ __launch_bounds__(kThreads, 2) void attn_tree_kernel(const TreeArgs a,
-                                                                const TreeSplit sp) {
+__global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeArgs a,
+                                                                    const TreeSplit sp) {
   constexpr bool Q8 = KIND != kCacheBf16;     // quantised
   constexpr int CB = Q8 ? 1 : 2;              // bytes of a code
   constexpr int T = Q8 ? 64 : 32;             // keys of a tile: 16 bytes of a feature per lane
@@ -169,248 +468,94 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_kernel(const TreeArgs a
   constexpr int NT = T / 16, NS = T / 32;     // operands of K, contraction steps of P V
   constexpr int KW = DQK * CB / 16;           // words of a K row a lane reads
   constexpr int KS = DQK / 32, NC = DV / 16;  // contraction steps of K Q^T, column tiles
-  __shared__ __attribute__((aligned(16))) Shared sh;
+  __shared__ __attribute__((aligned(16))) Keys<4> kb;
+  __shared__ Rows rs;
+  __shared__ short2 node[kMaxDraft];
   __shared__ float sums[2 * 16 * R * DV];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int H = a.ja.num_heads, lg = a.c.lg_page;
-  // Workgroups go to the eight dies in turn: the row blocks of one chunk and
-  // head group, which read the same keys, follow each other on one die.
-  const int die = blockIdx.x % 8, turn = blockIdx.x / 8;
-  const int rb = turn % sp.row_blocks;
-  const int unit = turn / sp.row_blocks * 8 + die;
-  const int hgs = H / sp.hg;
-  const int item = unit / hgs % sp.chunks, b = unit / hgs / sp.chunks;
-  if (b >= a.ja.num_seqs) return;
-  const int head0 = unit % hgs * sp.hg;
-  const int cap = a.c.max_pages << lg;
-  const int from = item * sp.chunk_len;
-  const int32_t* table = a.c.page_table + (int64_t)b * a.c.max_pages;
-
-  // What thread tid knows of key k0 + tid, fetched a block ahead.
-  int64_t key_page, key_time;
-  float key_ks[4], key_vs[4];
-  auto fetch_page = [&](int k0) { return k0 + tid < cap ? table[(k0 + tid) >> lg] : -1; };
-  const int first_page = fetch_page(from);
-  const int64_t o = a.ja.seq_offsets[b];
-  const int64_t o1 = min(a.ja.seq_offsets[b + 1], a.ja.total_tokens);
-  const int n_b = (int)max((int64_t)0, min(a.c.lengths[b], (int64_t)cap));
-  const int L = (int)max((int64_t)0, min(o1 - o, (int64_t)a.max_draft));
-  const int r0 = rb * sp.rows;
-  const int to = min(n_b, from + sp.chunk_len);
-  if (o < 0 || r0 >= L || from >= to) return;
-  auto fetch = [&](int k0, int page) {
-    const int place = (k0 + tid) & ((1 << lg) - 1);
-    key_page = k0 + tid < to && page < a.c.num_pages ? page : -1;
-    key_time = key_page >= 0 ? a.c.tc[(key_page << lg) + place] : 0;
-    if constexpr (Q8)
-#pragma unroll
-      for (int x = 0; x < 4; x++) {
-        const int64_t at = ((key_page * H + head0 + x) << lg) + place;
-        const bool on = key_page >= 0 && x < sp.hg;
-        key_ks[x] = on ? a.c.k_scale[at] : 0.0f;
-        key_vs[x] = on ? a.c.v_scale[at] : 0.0f;
-      }
-  };
-  fetch(from, first_page);
-
-  const int rows = min(sp.rows, L - r0);       // of the workgroup
-  const int nodes = r0 + rows;
-  // A wave's head, rows and share of the keys.
-  const int wr_count = sp.rows / (16 * R), ks_count = 4 / (sp.hg * wr_count);
-  const int hh = wave % sp.hg, wr = wave / sp.hg % wr_count, ks = wave / (sp.hg * wr_count);
-  const int head = head0 + hh;
-  const int w0 = wr * 16 * R;                  // its first row within the workgroup's
-  const bool idle = w0 >= rows;
+  Part w;
+  if (!find_part(a, sp, &w)) return;
+  const int lg = w.lg;
+  Ahead<4> h;
+  fetch<Q8>(a, w, w.from, fetch_page(a, w, w.from), &h);
+  // A wave's head and share of the keys.
+  const int ks_count = 4 / sp.hg, hh = wave % sp.hg, ks = wave / sp.hg;
+  const int head = w.head0 + hh;
   const int r = lane % 16, g = lane / 16;
-  const int N = a.ja.max_seq_len;
-
-  // Q as the right operand: row r of each group, in the order of feature().
   bf16x8 q[R][KS];
-#pragma unroll
-  for (int m = 0; m < R; m++) {
-    const int row = w0 + 16 * m + r;
-    const uint16_t* src =
-        (const uint16_t*)a.t.q + (o + r0 + row) * a.t.q_stride + (int64_t)head * DQK;
-#pragma unroll
-    for (int s = 0; s < KS; s++) {
-      u32x4 v = zero_u32x4();
-      if (row < rows) v = *reinterpret_cast<const u32x4*>(src + feature<KIND, DQK>(s, g));
-      q[m][s] = as_bf16x8(v);
-    }
-  }
+  load_q<KIND, DQK, R>(a, w, 0, head, q);
   f32x4 acc[R][NC];
 #pragma unroll
   for (int m = 0; m < R; m++)
 #pragma unroll
     for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
   for (int i = tid; i < a.ja.num_buckets; i += kThreads)
-    sh.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
-  if (tid < kMaxRows) sh.row_time[tid] = tid < rows ? a.ja.timestamps[o + r0 + tid] : 0;
-  // Depths of the rows (0 where there is none), and their extremes.
-  const int64_t* parents = a.parents ? a.parents + o : nullptr;
-  int depth[R], deep = 0, flat = 0;
-#pragma unroll
-  for (int m = 0; m < R; m++) depth[m] = 0;
-  if (parents) {
-    if (nodes <= 64) {
-      const int64_t p = lane < nodes ? parents[lane] : -1;
-      const int d = walk64(p >= 0 && p < lane ? (int)p : -1);
-#pragma unroll
-      for (int m = 0; m < R; m++) {
-        const int x = __shfl(d, (r0 + w0 + 16 * m + r) & 63, 64);
-        if (w0 + 16 * m + r < rows) depth[m] = x;
-      }
-      const bool own = lane >= r0 && lane < nodes;
-      deep = wave_extreme<true>(own ? d : 0);
-      flat = wave_extreme<false>(own ? d : kMaxDraft);
-    } else {
-      walk(parents, nodes, sh.node);
-      flat = kMaxDraft;
-      for (int i = r0 + lane; i < nodes; i += 64) {
-        deep = max(deep, (int)sh.node[i].y);
-        flat = min(flat, (int)sh.node[i].y);
-      }
-      deep = wave_extreme<true>(deep);
-      flat = wave_extreme<false>(flat);
-#pragma unroll
-      for (int m = 0; m < R; m++)
-        if (w0 + 16 * m + r < rows) depth[m] = sh.node[r0 + w0 + 16 * m + r].y;
-    }
-  }
-  const bool windowed = deep - flat < kWindow - kBlock;
-  // Where a row's window starts; a row that is not there takes the deepest's.
-  int shift[R];
-#pragma unroll
-  for (int m = 0; m < R; m++) shift[m] = windowed ? max(0, min(deep - depth[m], deep - flat)) : 0;
+    rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
+  if (tid < 16 * R) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  int depth[R];
+  find_depths<R>(a, &w, 0, node, depth);
+  fetch_pos(a, w, w.from, &h);
 
-  uint32_t kw[NT][KW];
-  uint32_t vw[NC][4];
-  for (int k0 = from; k0 < to; k0 += kBlock) {
-    const int keys = min(kBlock, to - k0);
+  u32x4 kw[NT][(KW + 3) / 4];
+  u32x4 vw[NC];
+  for (int k0 = w.from; k0 < w.to; k0 += kBlock) {
+    const int keys = min(kBlock, w.to - k0);
     __syncthreads();  // the block before is done with what follows
-    const bool ok = key_page >= 0;
-    if (tid % 16 == 0)
-      sh.rows16[tid / 16] =
-          ok ? ((key_page * H) << lg) + ((k0 + tid) & ((1 << lg) - 1)) : -1;
-    const int next_page = fetch_page(k0 + kBlock);
+    put_rows(a, w, k0, h, &kb);
+    const int next_page = fetch_page(a, w, k0 + kBlock);
     __syncthreads();
-    // Cached row of key `at` of the block for head 0, or -1.
-    auto row_of = [&](int at) {
-      const int64_t x = sh.rows16[at / 16];
-      return x < 0 ? x : x + at % 16;
-    };
-    auto load_k = [&](int t0, bool full) {
+    // The loads of a tile: always the same number, of rows that exist, so that a
+    // wait for one of them waits for nothing behind it.
+    auto load_k = [&](int t0) {
+      const int at = t0 + GK * (r / 4);  // operand t takes row at + 4 t + r % 4
+      const char* src = (const char*)a.c.kc + (kb.rows16[at / 16] + ((int64_t)head << lg) +
+                                               at % 16 + r % 4) * (DQK * CB);
 #pragma unroll
       for (int t = 0; t < NT; t++) {
-        const int at = t0 + GK * (r / 4) + 4 * t + r % 4;
-        const int64_t row = row_of(at);
-        const char* src = (const char*)a.c.kc + (row + ((int64_t)head << lg)) * (DQK * CB);
-        const bool on = full || (row >= 0 && at < keys);
         if constexpr (KW == 2) {
-          uint2 v{0u, 0u};
-          if (on) v = *reinterpret_cast<const uint2*>(src + 8 * g);
-          kw[t][0] = v.x;
-          kw[t][1] = v.y;
+          const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t * DQK * CB + 8 * g);
+          kw[t][0][0] = v.x;
+          kw[t][0][1] = v.y;
         } else {
 #pragma unroll
-          for (int u = 0; u < KW / 4; u++) {
-            u32x4 v = zero_u32x4();
-            if (on) v = *reinterpret_cast<const u32x4*>(src + 64 * u + 16 * g);
-#pragma unroll
-            for (int e = 0; e < 4; e++) kw[t][4 * u + e] = v[e];
-          }
+          for (int u = 0; u < KW / 4; u++)
+            kw[t][u] = *reinterpret_cast<const u32x4*>(src + 4 * t * DQK * CB + 64 * u + 16 * g);
         }
       }
     };
-    // How many of the keys of group g of a tile are there.
-    auto left_of = [&](int t0) {
+    auto load_v = [&](int t0) {
       const int at = t0 + GK * g;
-      return sh.rows16[at / 16] < 0 ? 0 : max(0, min(GK, keys - at));
-    };
-    auto load_v = [&](int t0, bool full) {
-      const int64_t row = row_of(t0 + GK * g);
-      const int place = (int)(row & ((1 << lg) - 1));
-      const int64_t ph = (row >> lg) + head;
-      const int left = full ? GK : left_of(t0);
+      const int64_t row = kb.rows16[at / 16];
+      const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
+      const char* src =
+          (const char*)a.c.vc + (((((row >> lg) + head) * DV + r) << lg) + place) * CB;
 #pragma unroll
-      for (int c = 0; c < NC; c++) {
-        const char* src = (const char*)a.c.vc + (((ph * DV + 16 * c + r) << lg) + place) * CB;
-        u32x4 v = zero_u32x4();
-        if (full || left > 0) v = *reinterpret_cast<const u32x4*>(src);
-        if (!full)
-#pragma unroll
-          for (int e = 0; e < 4; e++) {  // codes behind the last key count as zeros
-            const int keep = (left * CB - 4 * e) * 8;  // bits
-            v[e] = keep >= 32 ? v[e] : keep <= 0 ? 0u : v[e] & ((1u << keep) - 1u);
-          }
-#pragma unroll
-        for (int e = 0; e < 4; e++) vw[c][e] = v[e];
-      }
-    };
-    auto is_full = [&](int t0) {
-      bool yes = t0 + T <= keys;
-#pragma unroll
-      for (int x = 0; x < T / 16; x++) yes = yes && sh.rows16[t0 / 16 + x] >= 0;
-      return (bool)__builtin_amdgcn_readfirstlane(yes);
-    };
-    auto load = [&](int t0, auto part) {
-      if (is_full(t0)) part(t0, true);
-      else part(t0, false);
+      for (int c = 0; c < NC; c++)
+        vw[c] = *reinterpret_cast<const u32x4*>(src + ((int64_t)(16 * c * CB) << lg));
     };
     int t0 = ks * T;
-    const bool work = !idle && t0 < keys;
-    if (work) {
-      load(t0, load_k);
-      load(t0, load_v);
+    if (t0 < keys) {
+      load_k(t0);
+      load_v(t0);
     }
-    sh.time[tid] = key_time;
-    if constexpr (Q8)
-#pragma unroll
-      for (int x = 0; x < 4; x++)
-        if (x < sp.hg) {
-          sh.scales[0][x][tid] = key_ks[x] * kNegLog2e;
-          sh.scales[1][x][tid] = key_vs[x];
-        }
-    // The part of rab_pos that the block's pairs can reach: entry x belongs to
-    // x = key - k0 + deep - depth; copy c starts c entries later, so that any
-    // four in a row are one aligned read of some copy.
-    if (windowed) {
-      const int base = N - 1 + k0 - n_b - deep;
-#pragma unroll
-      for (int e = 0; e < kWindow / kThreads; e++) {
-        const int x = tid + e * kThreads;
-        if (x > kBlock + 2 + deep - flat) continue;
-        const float v = a.ja.rab_pos[max(0, min(2 * N - 2, base + x))] * kNegLog2e;
-#pragma unroll
-        for (int c = 0; c < 4; c++)
-          if (x >= c) sh.window[c][x - c] = v;
-      }
-    }
-    // What the rows' times have in common with those of this wave's 64 keys:
-    // |dt| is monotone in the key's time on either side of 0.
-    {
-      const int64_t lo = wave_extreme64<false>(ok ? key_time : INT64_MAX);
-      const int64_t hi = wave_extreme64<true>(ok ? key_time : INT64_MIN);
-      bool one = true, near = true;
-      for (int i = lane; lo <= hi && i < rows; i += 64) {
-        const int64_t x = sh.row_time[i] - lo, y = sh.row_time[i] - hi;
-        const int bx = time_bucket64(x, a.ja.num_buckets);
-        const int by = time_bucket64(y, a.ja.num_buckets);
-        one &= bx == by && ((x >= 0) == (y >= 0) || bx == 0);
-        near &= x == (int)x && y == (int)y && (int)x != INT32_MIN && (int)y != INT32_MIN;
-        sh.uniform[wave][i] = sh.rtime[by];
-      }
-      const bool all_one = __ballot(!one) == 0, all_near = __ballot(!near) == 0;
-      if (lane == 0) sh.times[wave] = all_one ? kTimesOne : all_near ? kTimesNear : kTimesAny;
-    }
+    put_keys<Q8>(a, w, rs, h, &kb);
     __syncthreads();
-    if (k0 + kBlock < to) fetch(k0 + kBlock, next_page);
-    if (!work) continue;
+    if (k0 + kBlock < w.to) {
+      fetch<Q8>(a, w, k0 + kBlock, next_page, &h);
+      fetch_pos(a, w, k0 + kBlock, &h);
+    }
     for (; t0 < keys; t0 += ks_count * T) {
-      const int next = t0 + ks_count * T;
-      const bool full = is_full(t0);
-      const int times = __builtin_amdgcn_readfirstlane(sh.times[t0 / 64]);
+      const int next = min(t0 + ks_count * T, kBlock - T);  // a tile too many is not used
+      const int about = __builtin_amdgcn_readfirstlane(kb.about[t0 / 64]);
+      const int all = Q8 ? 3 * kWhole : kWhole << (t0 / 32 % 2);
+      const bool whole = (about & all) == all;  // all keys are there
+      int left = GK;                            // keys of this lane's group
+      if (!whole) {
+        const int at = t0 + GK * g;
+        left = max(0, min(GK, kb.left16[at / 16] - at % 16));
+#pragma unroll
+        for (int c = 0; c < NC; c++) vw[c] = cut<CB>(vw[c], left);
+      }
 #pragma unroll
       for (int s = 0; s < NS; s++) {
         f32x4 sc[R][2];
@@ -422,83 +567,45 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_kernel(const TreeArgs a
 #pragma unroll
           for (int st = 0; st < KS; st++) {
             bf16x8 kf;
-            if constexpr (Q8) kf = widen<KIND>(kw[t][2 * st], kw[t][2 * st + 1]);
-            else kf = as_bf16x8(u32x4{kw[t][4 * st], kw[t][4 * st + 1], kw[t][4 * st + 2],
-                                      kw[t][4 * st + 3]});
+            if constexpr (Q8)
+              kf = widen<KIND>(kw[t][st / 2][st % 2 * 2], kw[t][st / 2][st % 2 * 2 + 1]);
+            else
+              kf = as_bf16x8(kw[t][st]);
 #pragma unroll
             for (int m = 0; m < R; m++) sc[m][x] = mfma16x16x32(kf, q[m][st], sc[m][x]);
           }
         }
-        if (s == NS - 1 && next < keys) load(next, load_k);
-        bf16x8 p[R];
-#pragma unroll
-        for (int m = 0; m < R; m++) {
-          const int row = w0 + 16 * m + r;
-          float w[8];
+        if (s == NS - 1) load_k(next);
+        const int at = t0 + GK * g + 8 * s;
+        f32x4 bv[R][2], kf[2], vf[2];
+        find_bias<4, R>(a, w, rs, kb, about, k0, at, 0, depth, bv);
+        if constexpr (Q8)
 #pragma unroll
           for (int x = 0; x < 2; x++) {
-            const int at = t0 + GK * g + 8 * s + 4 * x;
-            // -log2(e) times the bias of four pairs
-            f32x4 bv;
-            if (windowed) {
-              bv = *reinterpret_cast<const f32x4*>(
-                  &sh.window[shift[m] & 3][(shift[m] & ~3) + at]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; i++)
-                bv[i] =
-                    a.ja.rab_pos[max(0, N - 1 + k0 + at + i - n_b - depth[m])] * kNegLog2e;
-            }
-            if (times == kTimesOne) {
-              bv += sh.uniform[t0 / 64][row];
-            } else {
-              const int64_t rt = sh.row_time[row];
-#pragma unroll
-              for (int i = 0; i < 4; i++) {
-                int bucket;
-                if (times == kTimesNear) {
-                  const int dt = (int)rt - (int)sh.time[at + i];
-                  bucket = min(31 - __clz(max(1, max(dt, -dt))), a.ja.num_buckets - 1);
-                } else {
-                  bucket = time_bucket64(rt - sh.time[at + i], a.ja.num_buckets);
-                }
-                bv[i] += sh.rtime[bucket];
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-              float y;
-              if constexpr (Q8) y = fmaf(sc[m][x][i], sh.scales[0][hh][at + i], bv[i]);
-              else y = fmaf(sc[m][x][i], kNegLog2e, bv[i]);
-              y *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
-              if constexpr (Q8) y *= sh.scales[1][hh][at + i];
-              w[4 * x + i] = y;
-            }
+            kf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[0][hh][at + 4 * x]);
+            vf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[1][hh][at + 4 * x]);
           }
-          if (!full) {
-            const int left = left_of(t0) - 8 * s;
+        bf16x8 p[R];
 #pragma unroll
-            for (int i = 0; i < 8; i++) w[i] = i < left ? w[i] : 0.0f;
-          }
-          p[m] = as_bf16x8(pack_bf16x8(w));
-        }
+        for (int m = 0; m < R; m++)
+          p[m] = find_weights<Q8>(sc[m], bv[m], kf, vf, whole, left - 8 * s);
 #pragma unroll
         for (int c = 0; c < NC; c++) {
-          bf16x8 vf;
-          if constexpr (Q8) vf = widen<KIND>(vw[c][2 * s], vw[c][2 * s + 1]);
-          else vf = as_bf16x8(u32x4{vw[c][0], vw[c][1], vw[c][2], vw[c][3]});
+          bf16x8 vf8;
+          if constexpr (Q8) vf8 = widen<KIND>(vw[c][2 * s], vw[c][2 * s + 1]);
+          else vf8 = as_bf16x8(vw[c]);
 #pragma unroll
-          for (int m = 0; m < R; m++) acc[m][c] = mfma16x16x32(p[m], vf, acc[m][c]);
+          for (int m = 0; m < R; m++) acc[m][c] = mfma16x16x32(p[m], vf8, acc[m][c]);
         }
       }
-      if (next < keys) load(next, load_v);
+      load_v(next);
     }
   }
 
-  // The waves of a head and rows add up, in order.
+  // The waves of a head add up, in order.
   for (int x = 1; x < ks_count; x++) {
     __syncthreads();
-    float* space = sums + (wave % (4 / ks_count)) * (16 * R * DV);
+    float* space = sums + hh * (16 * R * DV);
     if (ks == x) {
 #pragma unroll
       for (int m = 0; m < R; m++)
@@ -519,17 +626,216 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_kernel(const TreeArgs a
             acc[m][c][i] += space[(16 * m + 4 * g + i) * DV + 16 * c + r];
     }
   }
-  if (ks != 0) return;
+  if (ks == 0) put_part<DV, R>(a, sp, w, 0, head, acc);
+}
+
+// A tile of one head in LDS.  K: rows of keys, V: rows of features, in 16-byte
+// pieces; a row's pieces are permuted so that the 16 rows that a quarter of a wave
+// reads one piece of lie in 16 different sixteenths of the banks.
+template <int KIND, int DQK, int DV>
+struct Tile {
+  static constexpr int CB = KIND != kCacheBf16 ? 1 : 2;
+  static constexpr int T = 64 / CB, GK = T / 4;
+  static constexpr int KP = DQK * CB / 16;  // pieces of a K row: 2, 4, 8 or 16
+  static constexpr int kPieces = T * KP, vPieces = DV * 4;
+  char k[kPieces * 16];
+  char v[vPieces * 16];
+
+  __device__ static int k_at(int key, int piece) {
+    // rows key % 4 + GK (0..3) are read together, 16 / KP of them side by side in
+    // the banks
+    const int low = KP == 16 ? key & 3 : KP == 8 ? key >> 1 & 1 : 0;
+    const int high = (key / GK) & 3;
+    const int turn = (KP == 16 ? low | high << 2 : KP == 8 ? low | high << 1 : high) & (KP - 1);
+    return (key * KP + (piece ^ turn)) * 16;
+  }
+  __device__ static int v_at(int f, int piece) { return (f * 4 + (piece ^ (f >> 2 & 3))) * 16; }
+};
+
+template <int KIND, int DQK, int DV, int R>
+__global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeArgs a,
+                                                                     const TreeSplit sp) {
+  using Tl = Tile<KIND, DQK, DV>;
+  constexpr bool Q8 = KIND != kCacheBf16;
+  constexpr int CB = Tl::CB, T = Tl::T, GK = Tl::GK, KP = Tl::KP;
+  constexpr int NS = T / 32, KS = DQK / 32, NC = DV / 16;
+  constexpr int KL = (Tl::kPieces + kThreads - 1) / kThreads;  // pieces a thread loads
+  constexpr int VL = (Tl::vPieces + kThreads - 1) / kThreads;
+  constexpr int TB = kBlock / T;                               // tiles of a block
+  __shared__ __attribute__((aligned(16))) Keys<1> kb[2];
+  __shared__ __attribute__((aligned(16))) Tl tiles[2];
+  __shared__ Rows rs;
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  Part w;
+  if (!find_part(a, sp, &w)) return;
+  const int lg = w.lg, head = w.head0;
+  Ahead<1> h;
+  fetch<Q8>(a, w, w.from, fetch_page(a, w, w.from), &h);
+  const int w0 = wave * 16 * R;  // the wave's first row within the workgroup's
+  const bool idle = w0 >= w.rows;
+  const int r = lane % 16, g = lane / 16;
+  bf16x8 q[R][KS];
+  load_q<KIND, DQK, R>(a, w, w0, head, q);
+  f32x4 acc[R][NC];
 #pragma unroll
   for (int m = 0; m < R; m++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int row = w0 + 16 * m + 4 * g + i;
-      if (row >= rows) continue;
-      float* dst = sp.part + (((int64_t)item * a.ja.total_tokens + o + r0 + row) * H + head) * DV + r;
+    for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = tid; i < a.ja.num_buckets; i += kThreads)
+    rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
+  if (tid < kMaxRows) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  int depth[R];
+  static_assert(sizeof(tiles) >= kMaxDraft * sizeof(short2), "the depths fit where the tiles go");
+  find_depths<R>(a, &w, w0, reinterpret_cast<short2*>(tiles), depth);
+  fetch_pos(a, w, w.from, &h);
+  __syncthreads();
+  put_rows(a, w, w.from, h, &kb[0]);
+  put_keys<Q8>(a, w, rs, h, &kb[0]);
+  if (w.from + kBlock < w.to) {
+    fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
+    fetch_pos(a, w, w.from + kBlock, &h);
+  }
+  __syncthreads();
+
+  // Tile j of the chunk: loads into registers, then into LDS.
+  const int count = (w.to - w.from + T - 1) / T;
+  u32x4 kr[KL], vr[VL];
+  auto load = [&](int j) {
+    const Keys<1>& k = kb[j / TB % 2];
+    const int t0 = j % TB * T;
 #pragma unroll
-      for (int c = 0; c < NC; c++) dst[16 * c] = acc[m][c][i];
+    for (int e = 0; e < KL; e++) {
+      const int x = tid + e * kThreads, at = t0 + x / KP;
+      if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
+      kr[e] = *reinterpret_cast<const u32x4*>(
+          (const char*)a.c.kc +
+          (k.rows16[at / 16] + ((int64_t)head << lg) + at % 16) * (DQK * CB) + x % KP * 16);
     }
+#pragma unroll
+    for (int e = 0; e < VL; e++) {
+      const int x = tid + e * kThreads, at = t0 + GK * (x % 4);
+      if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
+      const int64_t row = k.rows16[at / 16];
+      const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
+      vr[e] = *reinterpret_cast<const u32x4*>(
+          (const char*)a.c.vc + (((((row >> lg) + head) * DV + x / 4) << lg) + place) * CB);
+    }
+  };
+  auto is_whole = [&](int j) {
+    const int t0 = j % TB * T, all = Q8 ? 3 * kWhole : kWhole << (t0 / 32 % 2);
+    const int about = __builtin_amdgcn_readfirstlane(kb[j / TB % 2].about[t0 / 64]);
+    return (about & all) == all;
+  };
+  auto store = [&](int j) {
+    Tl& tl = tiles[j % 2];
+#pragma unroll
+    for (int e = 0; e < KL; e++) {
+      const int x = tid + e * kThreads;
+      if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
+      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[e];
+    }
+    if (!is_whole(j)) {  // codes behind the last key count as zeros
+      const Keys<1>& k = kb[j / TB % 2];
+      const int at = j % TB * T + GK * (tid % 4);
+      const int left = max(0, min(GK, k.left16[at / 16] - at % 16));
+#pragma unroll
+      for (int e = 0; e < VL; e++) vr[e] = cut<CB>(vr[e], left);
+    }
+#pragma unroll
+    for (int e = 0; e < VL; e++) {
+      const int x = tid + e * kThreads;
+      if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
+      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4, x % 4)) = vr[e];
+    }
+  };
+  load(0);
+  store(0);
+  __syncthreads();
+  for (int j = 0; j < count; j++) {
+    const bool more = j + 1 < count;
+    if (more) load(j + 1);
+    // the next block's keys, two tiles before they are needed
+    const int k1 = w.from + (j / TB + 1) * kBlock;
+    if (j % TB == TB - 3 && k1 < w.to) {
+      put_rows(a, w, k1, h, &kb[(j / TB + 1) % 2]);
+      put_keys<Q8>(a, w, rs, h, &kb[(j / TB + 1) % 2]);
+      if (k1 + kBlock < w.to) {
+        fetch<Q8>(a, w, k1 + kBlock, fetch_page(a, w, k1 + kBlock), &h);
+        fetch_pos(a, w, k1 + kBlock, &h);
+      }
+    }
+    if (!idle) {
+      const Keys<1>& k = kb[j / TB % 2];
+      const Tl& tl = tiles[j % 2];
+      const int t0 = j % TB * T, k0 = w.from + j / TB * kBlock;
+      const int about = __builtin_amdgcn_readfirstlane(k.about[t0 / 64]);
+      const bool whole = is_whole(j);
+      int left = GK;  // keys of this lane's group
+      if (!whole) {
+        const int at = t0 + GK * g;
+        left = max(0, min(GK, k.left16[at / 16] - at % 16));
+      }
+#pragma unroll
+      for (int s = 0; s < NS; s++) {
+        f32x4 sc[R][2];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          const int t = 2 * s + x, key = GK * (r / 4) + 4 * t + r % 4;
+#pragma unroll
+          for (int m = 0; m < R; m++) sc[m][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          auto step = [&](int st, bf16x8 kf) {
+#pragma unroll
+            for (int m = 0; m < R; m++) sc[m][x] = mfma16x16x32(kf, q[m][st], sc[m][x]);
+          };
+          if constexpr (Q8 && DQK == 32) {
+            const uint2 c =
+                *reinterpret_cast<const uint2*>(tl.k + Tl::k_at(key, g / 2) + 8 * (g % 2));
+            step(0, widen<KIND>(c.x, c.y));
+          } else {
+#pragma unroll
+            for (int u = 0; u < KP / 4; u++) {
+              const u32x4 c = *reinterpret_cast<const u32x4*>(tl.k + Tl::k_at(key, 4 * u + g));
+              if constexpr (Q8) {
+                step(2 * u, widen<KIND>(c[0], c[1]));
+                step(2 * u + 1, widen<KIND>(c[2], c[3]));
+              } else {
+                step(u, as_bf16x8(c));
+              }
+            }
+          }
+        }
+        const int at = t0 + GK * g + 8 * s;
+        f32x4 bv[R][2], kf[2], vf[2];
+        find_bias<1, R>(a, w, rs, k, about, k0, at, w0, depth, bv);
+        if constexpr (Q8)
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            kf[x] = *reinterpret_cast<const f32x4*>(&k.scales[0][0][at + 4 * x]);
+            vf[x] = *reinterpret_cast<const f32x4*>(&k.scales[1][0][at + 4 * x]);
+          }
+        bf16x8 p[R];
+#pragma unroll
+        for (int m = 0; m < R; m++)
+          p[m] = find_weights<Q8>(sc[m], bv[m], kf, vf, whole, left - 8 * s);
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+          bf16x8 v8;
+          const char* src = tl.v + Tl::v_at(16 * c + r, g);
+          if constexpr (Q8) {
+            const uint2 x = *reinterpret_cast<const uint2*>(src + 8 * s);
+            v8 = widen<KIND>(x.x, x.y);
+          } else {
+            v8 = as_bf16x8(*reinterpret_cast<const u32x4*>(src));
+          }
+#pragma unroll
+          for (int m = 0; m < R; m++) acc[m][c] = mfma16x16x32(p[m], v8, acc[m][c]);
+        }
+      }
+    }
+    if (more) store(j + 1);
+    __syncthreads();
+  }
+  if (!idle) put_part<DV, R>(a, sp, w, w0, head, acc);
 }
 
 // The launch for one kind of cache.
@@ -541,9 +847,11 @@ hipError_t launch(const TreeArgs& a, const TreeSplit& sp, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, sp);
     return hipGetLastError();
   };
-#define HSTU_TREE_R(DQK, DV)                                        \
-  if (sp.rows == 16) return go(attn_tree_kernel<KIND, DQK, DV, 1>); \
-  return go(attn_tree_kernel<KIND, DQK, DV, 2>);
+#define HSTU_TREE_R(DQK, DV)                                             \
+  if (sp.rows == 16) return go(attn_tree_few_kernel<KIND, DQK, DV, 1>);  \
+  if (sp.rows == 32) return go(attn_tree_few_kernel<KIND, DQK, DV, 2>);  \
+  if (sp.rows == 64) return go(attn_tree_many_kernel<KIND, DQK, DV, 1>); \
+  return go(attn_tree_many_kernel<KIND, DQK, DV, 2>);
 #define HSTU_TREE_DV(DQK)                       \
   if (a.d_v == 32) { HSTU_TREE_R(DQK, 32) }     \
   if (a.d_v == 64) { HSTU_TREE_R(DQK, 64) }     \

@@ -196,8 +196,8 @@ TreeSplit tree_split(int32_t num_seqs, int64_t total_tokens, int32_t num_heads, 
       std::min((int64_t)num_seqs * sp.row_blocks, total_tokens / sp.rows + num_seqs);
   const int64_t keys = std::min(cap, (int64_t)max_seq_len);
   const int64_t most = (keys + tree::kBlock - 1) / tree::kBlock;
-  // Four waves: heads, rows in 32s, then shares of the keys.
-  sp.hg = sp.rows > 64 ? 1 : sp.rows > 32 ? 2 : 4;
+  // Four waves: heads and shares of the keys, or rows of one head.
+  sp.hg = sp.rows > 32 ? 1 : 4;
   while (num_heads % sp.hg) sp.hg /= 2;
   while (sp.hg > 1 && blocks * (num_heads / sp.hg) * most < kWanted) sp.hg /= 2;
   const int64_t base = blocks * (num_heads / sp.hg);
