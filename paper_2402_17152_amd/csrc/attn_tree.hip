@@ -10,35 +10,75 @@ namespace {
 
 using tree::kThreads;
 
-constexpr int kLevels = 10;  // ways of up to 2^10 nodes
+// A forest that the rows' ways to the roots are found in: up(l, i) is the node 2^l
+// steps above node i, or -1.  levels: how many of them are in use.
 
-// Places in a forest: up[l][i] is the node 2^l steps above node i, or -1.
-struct Ways {
-  short up[kLevels][kMaxDraft];
+// All nodes are roots.
+struct FlatForest {
+  static constexpr int levels = 0;
+  __device__ FlatForest(const TreeArgs&, int64_t, int, short*) {}
+  __device__ int up(int, int) const { return -1; }
+  __device__ int64_t time(const TreeArgs& a, int64_t o, int n) const {
+    return a.ja.timestamps[o + n];
+  }
 };
 
-// Fills the ways of the nodes below n; returns the number of levels in use (the
-// same for all threads).  Ends past a barrier.
-__device__ __forceinline__ int climb(const int64_t* parents, int n, Ways* w) {
-  bool more = false;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int64_t p = parents[i];
-    const short x = p >= 0 && p < i ? (short)p : (short)-1;
-    w->up[0][i] = x;
-    more |= x >= 0;
-  }
-  int l = 0;
-  while (__syncthreads_or(more) && ++l < kLevels) {
-    more = false;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const short x = w->up[l - 1][i];
-      const short y = x >= 0 ? w->up[l - 1][x] : (short)-1;
-      w->up[l][i] = y;
-      more |= y >= 0;
+// Up to 64 nodes, node l in lane l of every wave, without LDS and barriers.
+struct LaneForest {
+  static constexpr int kMost = 6;
+  int levels = 0, ways[kMost];
+  int64_t times;
+  __device__ LaneForest(const TreeArgs& a, int64_t o, int n, short*) {
+    const int lane = __lane_id();
+    const int64_t p = lane < n ? a.parents[o + lane] : -1;
+    times = lane < n ? a.ja.timestamps[o + lane] : 0;
+    int x = p >= 0 && p < lane ? (int)p : -1;
+#pragma unroll
+    for (int l = 0; l < kMost; l++) {
+      ways[l] = x;
+      if (__ballot(x >= 0)) levels = l + 1;
+      const int y = __shfl(x, x >= 0 ? x : lane, 64);
+      x = x >= 0 ? y : -1;
     }
   }
-  return l;
-}
+  __device__ int up(int l, int n) const {
+    int w = ways[0];
+#pragma unroll
+    for (int k = 1; k < kMost; k++) w = l == k ? ways[k] : w;
+    return __shfl(w, n, 64);
+  }
+  __device__ int64_t time(const TreeArgs&, int64_t, int n) const { return __shfl(times, n, 64); }
+};
+
+// Any number of nodes, in LDS: [level][max_draft].
+struct LdsForest {
+  int levels = 0, ld;
+  const short* ways;
+  __device__ LdsForest(const TreeArgs& a, int64_t o, int n, short* space)
+      : ld(a.max_draft), ways(space) {
+    bool more = false;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const int64_t p = a.parents[o + i];
+      const short x = p >= 0 && p < i ? (short)p : (short)-1;
+      space[i] = x;
+      more |= x >= 0;
+    }
+    // a way has at most n - 1 steps: no level with 2^l >= n is in use
+    while (__syncthreads_or(more) && 1 << ++levels < n) {
+      more = false;
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const short x = space[(levels - 1) * ld + i];
+        const short y = x >= 0 ? space[(levels - 1) * ld + x] : (short)-1;
+        space[levels * ld + i] = y;
+        more |= y >= 0;
+      }
+    }
+  }
+  __device__ int up(int l, int n) const { return ways[l * ld + n]; }
+  __device__ int64_t time(const TreeArgs& a, int64_t o, int n) const {
+    return a.ja.timestamps[o + n];
+  }
+};
 
 __device__ __forceinline__ void add8(float* x, u32x4 v, float w) {
 #pragma unroll
@@ -54,12 +94,12 @@ __device__ __forceinline__ void add8(float* x, u32x4 v, float w) {
 // so several of them are under way at once.  Latency-bound for few rows, then
 // bound by the partial outputs' bytes.  Where there are many chunks the four waves
 // of a workgroup share a row and head (`waves` 4).
-template <int DQK, int DV>
+template <int DQK, int DV, typename Forest>
 __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
                                                                const TreeSplit sp, int per,
                                                                int waves) {
   constexpr int LK = DQK / 8, LV = DV / 8;  // lanes of a K row, of a V row
-  __shared__ Ways ways;
+  extern __shared__ short space[];
   __shared__ float weight[kThreads / 64][64];
   __shared__ float rest[kThreads / 64 - 1][DV];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -68,13 +108,13 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
   const int b = blockIdx.x / blocks, r0 = blockIdx.x % blocks * per;
   const int64_t o = a.ja.seq_offsets[b];
   const int64_t o1 = min(a.ja.seq_offsets[b + 1], a.ja.total_tokens);
-  const int L = (int)max((int64_t)0, min(o1 - o, (int64_t)a.max_draft));
-  if (o < 0 || r0 >= L) return;
   const int64_t cap = (int64_t)a.c.max_pages << a.c.lg_page;
   const int64_t n_b = max((int64_t)0, min(a.c.lengths[b], cap));
+  const int L = (int)max((int64_t)0, min(o1 - o, (int64_t)a.max_draft));
+  if (o < 0 || r0 >= L) return;
   const int used = (int)((n_b + sp.chunk_len - 1) / sp.chunk_len);
   const int rows = min(per, L - r0);
-  const int levels = a.parents ? climb(a.parents + o, r0 + rows, &ways) : 0;
+  const Forest forest(a, o, r0 + rows, space);
   const int N = a.ja.max_seq_len;
   const int share = waves == 1 ? 0 : wave;  // of the chunks
   const int pairs = rows * (waves == 1 ? H : 1);
@@ -82,6 +122,35 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
     const int i = r0 + (waves == 1 ? pair / H : pair);
     const int head = waves == 1 ? pair % H : blockIdx.y;
     const int64_t t = o + i;
+    const u32x4 q8 = *reinterpret_cast<const u32x4*>(
+        (const uint16_t*)a.t.q + t * a.t.q_stride + head * DQK + 8 * (lane % LK));
+    auto key = [&](int n) {
+      return *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.k + (o + n) * a.t.k_stride +
+                                             head * DQK + 8 * (lane % LK));
+    };
+    auto value = [&](int n) {
+      return *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.v + (o + n) * a.t.v_stride +
+                                             head * DV + 8 * (lane % LV));
+    };
+    int count = 1;  // nodes on the way, this one included
+    for (int l = forest.levels - 1, n = i; l >= 0; l--) {
+      const int m = forest.up(l, n);
+      if (m >= 0) {
+        count += 1 << l;
+        n = m;
+      }
+    }
+    auto above = [&](int steps) {
+      int n = i;
+      for (int l = 0; l < forest.levels; l++) {
+        const int m = forest.up(l, n);
+        if ((steps >> l) & 1) n = m;
+      }
+      return n;
+    };
+    // The first of the values, on its way while the weights are found.
+    const int first = above(min(lane / LV, count - 1));
+    const u32x4 v8 = value(first);
     float x[8] = {};
     {
       const int64_t slot = a.ja.total_tokens * H * DV;
@@ -102,43 +171,33 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
       for (int e = 0; e < 8; e++) x[e] *= -0.6931471805599453f;
     }
     if (share == 0) {
-      int count = 1;  // nodes on the way, this one included
-      for (int l = levels - 1, n = i; l >= 0; l--)
-        if (ways.up[l][n] >= 0) {
-          count += 1 << l;
-          n = ways.up[l][n];
-        }
-      auto above = [&](int steps) {
-        int n = i;
-        for (int l = 0; l < levels; l++)
-          if ((steps >> l) & 1) n = ways.up[l][n];
-        return n;
-      };
       float q[8] = {};
-      add8(q, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.q + t * a.t.q_stride +
-                                              head * DQK + 8 * (lane % LK)), 1.0f);
-      const int64_t time = a.ja.timestamps[t];
+      add8(q, q8, 1.0f);
+      const int64_t time = forest.time(a, o, i);
       for (int w0 = 0; w0 < count; w0 += 64) {
         const int here = min(64, count - w0);
-        for (int y = lane / LK; y < here; y += 64 / LK) {
-          const int64_t n = o + above(w0 + y);
+        for (int y0 = 0; y0 < here; y0 += 64 / LK) {
+          const int y = min(y0 + lane / LK, here - 1);
+          const int n = above(w0 + y);
+          const int64_t dt = time - forest.time(a, o, n);
           float k[8] = {};
-          add8(k, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.k + n * a.t.k_stride +
-                                                  head * DQK + 8 * (lane % LK)), 1.0f);
+          add8(k, key(n), 1.0f);
           float s = 0.0f;
 #pragma unroll
           for (int e = 0; e < 8; e++) s = fmaf(q[e], k[e], s);
 #pragma unroll
           for (int m = 1; m < LK; m *= 2) s += __shfl_xor(s, m, 64);
           s += a.ja.rab_pos[max(0, N - 1 - (w0 + y))] +
-               a.ja.rab_time[time_bucket64(time - a.ja.timestamps[n], a.ja.num_buckets)];
-          if (lane % LK == 0) weight[wave][y] = s * sigmoid_fast(s);
+               a.ja.rab_time[time_bucket64(dt, a.ja.num_buckets)];
+          if (lane % LK == 0 && y0 + lane / LK < here) weight[wave][y] = s * sigmoid_fast(s);
         }
         __builtin_amdgcn_wave_barrier();
-        for (int y = lane / LV; y < here; y += 64 / LV)
-          add8(x, *reinterpret_cast<const u32x4*>((const uint16_t*)a.t.v +
-                                                  (o + above(w0 + y)) * a.t.v_stride +
-                                                  head * DV + 8 * (lane % LV)), weight[wave][y]);
+        for (int y0 = 0; y0 < here; y0 += 64 / LV) {
+          const int y = y0 + lane / LV;
+          const bool on = y < here;
+          const u32x4 v = w0 + y0 == 0 ? v8 : value(above(w0 + min(y, here - 1)));
+          if (on) add8(x, v, weight[wave][y]);
+        }
         __builtin_amdgcn_wave_barrier();
       }
     }
@@ -212,22 +271,33 @@ hipError_t launch_attn_tree(const TreeArgs& a, const TreeSplit& sp, int kind, hi
                  : kind == kCacheE4m3 ? tree::launch_e4m3(a, sp, s)
                                       : tree::launch_int8(a, sp, s);
   if (e != hipSuccess) return e;
+  // Rows of a workgroup: one, while there are few of them.
   const int waves = sp.chunks > 16 ? 4 : 1;
-  const int per = waves == 4 ? 1 : std::min(4, a.max_draft);
+  const int64_t T = a.ja.total_tokens;
+  const int per = waves == 4 || T < 4096 ? 1 : T < 8192 ? 2 : 4;
   const dim3 grid((unsigned)((int64_t)a.ja.num_seqs * ((a.max_draft + per - 1) / per)),
                   waves == 4 ? (unsigned)a.ja.num_heads : 1u);
+  size_t space = 0;
+  if (a.parents && a.max_draft > 64)
+    for (int l = 0; l == 0 || 1 << l < a.max_draft; l++)
+      space += (size_t)a.max_draft * sizeof(short);
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, sp, per, waves);
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), space, s, a, sp, per, waves);
     return hipGetLastError();
   };
-#define HSTU_FINISH_DV(DQK)                                    \
-  return a.d_v == 32   ? go(tree_finish_kernel<DQK, 32>)       \
-         : a.d_v == 64 ? go(tree_finish_kernel<DQK, 64>)       \
-                       : go(tree_finish_kernel<DQK, 128>);
+#define HSTU_FINISH(DQK, DV)                                                        \
+  return !a.parents          ? go(tree_finish_kernel<DQK, DV, FlatForest>)          \
+         : a.max_draft <= 64 ? go(tree_finish_kernel<DQK, DV, LaneForest>)          \
+                             : go(tree_finish_kernel<DQK, DV, LdsForest>);
+#define HSTU_FINISH_DV(DQK)                 \
+  if (a.d_v == 32) { HSTU_FINISH(DQK, 32) } \
+  if (a.d_v == 64) { HSTU_FINISH(DQK, 64) } \
+  HSTU_FINISH(DQK, 128)
   if (a.d_qk == 32) { HSTU_FINISH_DV(32) }
   if (a.d_qk == 64) { HSTU_FINISH_DV(64) }
   HSTU_FINISH_DV(128)
 #undef HSTU_FINISH_DV
+#undef HSTU_FINISH
 }
 
 hipError_t launch_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_t max_draft,
