@@ -784,6 +784,7 @@ hstu_status_t hstu_attn_fwd_tree(const hstu_problem_t* p, const hstu_jagged_t* j
     a.d_v = p->d_v;
     a.out = out;
     sp.part = (float*)ws;
+    sp.last = sp.chunks == 1 && (!parents || max_draft == 1);
     TimedScope ts("attn_fwd_tree", s);
     HSTU_HIP(launch_attn_tree(a, sp, cache_kind(c), s), "attn_fwd_tree launch");
     return ok();

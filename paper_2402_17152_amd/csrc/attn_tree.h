@@ -13,7 +13,8 @@
 //   in lane l.  That is the layout of the weights as the left operand of O = P V,
 //   whose contraction runs over keys T/4 g + 8 s + 0..7: no exchange between lanes.
 //   The cache holds V transposed, so its operand (T/4 keys of a feature) is 16 bytes
-//   in a row.
+//   in a row.  Column r of V's operand c is feature d_v / 16 r + c: a lane's outputs
+//   of a row lie side by side.
 //
 // Codes of 8 bits are exact in bf16; a key's scales multiply the score and the
 // weight.  Everything is kept times -log2(e): y = -log2(e) s gives SiLU(s) =
@@ -165,13 +166,17 @@ __device__ __forceinline__ int wave_extreme(int v) {
   return __builtin_amdgcn_readlane(v, 63);
 }
 
+// The same for the 64-bit values of the lanes with `on`; those of all lanes often
+// have the same high word.
 template <bool MAX>
-__device__ __forceinline__ int64_t wave_extreme64(int64_t v) {
-  const int hi = (int)(v >> 32);
-  const int top = wave_extreme<MAX>(hi);
-  // the low words compare as unsigned numbers
+__device__ __forceinline__ int64_t wave_extreme64(int64_t v, bool on) {
   const int none = MAX ? INT32_MIN : INT32_MAX;
-  const int lo = wave_extreme<MAX>(hi == top ? (int)((uint32_t)v ^ 0x80000000u) : none);
+  const int hi = on ? (int)(v >> 32) : none;
+  const uint64_t lanes = __ballot(on);
+  int top = __builtin_amdgcn_readlane(hi, lanes ? __builtin_ctzll(lanes) : 0);
+  if (__ballot(on && hi != top)) top = wave_extreme<MAX>(hi);
+  // the low words compare as unsigned numbers
+  const int lo = wave_extreme<MAX>(on && hi == top ? (int)((uint32_t)v ^ 0x80000000u) : none);
   return (int64_t)top << 32 | (uint32_t)(lo ^ (int)0x80000000u);
 }
 
@@ -182,12 +187,12 @@ struct Part {
   int64_t o;               // first drafted token of the user
   int r0, rows;            // drafted rows: r0 .. r0 + rows - 1 of the user's
   int n_b, cap, lg;        // cached tokens, room for them, log2 of the page size
-  int deep, flat;          // depths of the rows: the largest, the smallest
+  int deep;                // the largest depth that the window is for
   bool windowed;           // Keys::window holds all that the rows reach
 };
 
-// The user, rows and keys of a workgroup; false: there is nothing to do.
-__device__ __forceinline__ bool find_part(const TreeArgs& a, const TreeSplit& sp, Part* w) {
+// The user, heads and chunk of a workgroup; false: there are none.
+__device__ __forceinline__ bool find_place(const TreeArgs& a, const TreeSplit& sp, Part* w) {
   // Workgroups go to the eight dies in turn: the row blocks of one chunk and
   // head group, which read the same keys, follow each other on one die.
   const int die = blockIdx.x % 8, turn = blockIdx.x / 8;
@@ -202,14 +207,19 @@ __device__ __forceinline__ bool find_part(const TreeArgs& a, const TreeSplit& sp
   w->lg = a.c.lg_page;
   w->cap = a.c.max_pages << w->lg;
   w->from = item * sp.chunk_len;
+  w->r0 = rb * sp.rows;
+  return true;
+}
+
+// Its rows and keys; false: there is nothing to do.
+__device__ __forceinline__ bool find_part(const TreeArgs& a, const TreeSplit& sp, Part* w) {
   w->o = a.ja.seq_offsets[w->b];
   const int64_t o1 = min(a.ja.seq_offsets[w->b + 1], a.ja.total_tokens);
   w->n_b = (int)max((int64_t)0, min(a.c.lengths[w->b], (int64_t)w->cap));
   const int L = (int)max((int64_t)0, min(o1 - w->o, (int64_t)a.max_draft));
-  w->r0 = rb * sp.rows;
   w->to = min(w->n_b, w->from + sp.chunk_len);
   w->rows = min(sp.rows, L - w->r0);
-  return w->o >= 0 && w->r0 < L && w->from < w->to;
+  return w->o >= 0 && w->r0 < L && (w->from < w->to || (sp.last && w->from == 0));
 }
 
 // What a thread knows of key k0 + its number, before it is in LDS.
@@ -224,11 +234,15 @@ __device__ __forceinline__ int fetch_page(const TreeArgs& a, const Part& w, int 
   return j < w.cap ? a.c.page_table[(int64_t)w.b * a.c.max_pages + (j >> w.lg)] : -1;
 }
 
+__device__ __forceinline__ int64_t valid_page(const TreeArgs& a, const Part& w, int k0, int page) {
+  return k0 + (int)threadIdx.x < w.to && page < a.c.num_pages ? page : -1;
+}
+
 template <bool Q8, int HG>
 __device__ __forceinline__ void fetch(const TreeArgs& a, const Part& w, int k0, int page,
                                       Ahead<HG>* h) {
-  const int j = k0 + (int)threadIdx.x, place = j & ((1 << w.lg) - 1);
-  h->page = j < w.to && page < a.c.num_pages ? page : -1;
+  const int place = (k0 + (int)threadIdx.x) & ((1 << w.lg) - 1);
+  h->page = valid_page(a, w, k0, page);
   h->time = h->page >= 0 ? a.c.tc[(h->page << w.lg) + place] : 0;
   if constexpr (Q8)
 #pragma unroll
@@ -254,13 +268,13 @@ __device__ __forceinline__ void fetch_pos(const TreeArgs& a, const Part& w, int 
 // Where the rows of a block's keys are.
 template <int HG>
 __device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k0,
-                                         const Ahead<HG>& h, Keys<HG>* k) {
-  const uint64_t there = __ballot(h.page >= 0);
+                                         int64_t page, Keys<HG>* k) {
+  const uint64_t there = __ballot(page >= 0);
   const int tid = threadIdx.x;
   if (tid % 16 == 0) {
     // keys of 16 lie on one page, the last ones may be missing
     k->rows16[tid / 16] =
-        h.page >= 0 ? ((h.page * a.ja.num_heads) << w.lg) + ((k0 + tid) & ((1 << w.lg) - 1)) : 0;
+        page >= 0 ? ((page * a.ja.num_heads) << w.lg) + ((k0 + tid) & ((1 << w.lg) - 1)) : 0;
     k->left16[tid / 16] = __popc((uint32_t)(there >> (tid % 64)) & 0xffffu);
   }
 }
@@ -292,10 +306,10 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
   // |dt| is monotone in the key's time on either side of 0.
   const bool ok = h.page >= 0;
   const uint64_t there = __ballot(ok);
-  const int64_t lo = wave_extreme64<false>(ok ? h.time : INT64_MAX);
-  const int64_t hi = wave_extreme64<true>(ok ? h.time : INT64_MIN);
+  const int64_t lo = wave_extreme64<false>(h.time, ok);
+  const int64_t hi = wave_extreme64<true>(h.time, ok);
   bool one = true, near = true;
-  for (int i = lane; lo <= hi && i < w.rows; i += 64) {
+  for (int i = lane; there && i < w.rows; i += 64) {
     const int64_t x = rows.time[i] - lo, y = rows.time[i] - hi;
     const int bx = time_bucket64(x, a.ja.num_buckets);
     const int by = time_bucket64(y, a.ja.num_buckets);
@@ -310,42 +324,52 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
   if (lane == 0) k->about[wave] = all_one | all_near | whole;
 }
 
-// Depths of this lane's rows w0 + 16 m + r (0 where there is none), and the extremes
-// of all rows.  Ends past a barrier if `node` is used.
+// The depths that the window covers, where max_draft says enough: it then does not
+// wait for the depths themselves.
+__device__ __forceinline__ bool bound_depths(const TreeArgs& a, Part* w) {
+  w->windowed = a.max_draft <= kWindow - kBlock || !a.parents;
+  w->deep = a.parents ? a.max_draft - 1 : 0;
+  return w->windowed;
+}
+
+// Depths of this lane's rows w0 + 16 m + r (0 where there is none), and, where
+// bound_depths() does not know them, the window's.
 template <int R>
 __device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, short2* node,
                                             int* depth) {
   const int lane = threadIdx.x % 64, r = lane % 16;
-  const int64_t* parents = a.parents ? a.parents + w->o : nullptr;
   const int nodes = w->r0 + w->rows;
-  w->deep = w->flat = 0;
 #pragma unroll
   for (int m = 0; m < R; m++) depth[m] = 0;
-  if (parents) {
+  if (!a.parents) return;
+  const int64_t* parents = a.parents + w->o;
+  if (nodes <= 64) {
+    const int64_t p = lane < nodes ? parents[lane] : -1;
+    const int d = walk64(p >= 0 && p < lane ? (int)p : -1);
+#pragma unroll
+    for (int m = 0; m < R; m++) {
+      const int x = __shfl(d, (w->r0 + w0 + 16 * m + r) & 63, 64);
+      if (w0 + 16 * m + r < w->rows) depth[m] = x;
+    }
+    if (!w->windowed) {  // depths below 64
+      w->windowed = true;
+      w->deep = 63;
+    }
+    return;
+  }
+  walk(parents, nodes, node);
+#pragma unroll
+  for (int m = 0; m < R; m++)
+    if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
+  if (!w->windowed) {
     int deep = 0, flat = kMaxDraft;
-    if (nodes <= 64) {
-      const int64_t p = lane < nodes ? parents[lane] : -1;
-      const int d = walk64(p >= 0 && p < lane ? (int)p : -1);
-#pragma unroll
-      for (int m = 0; m < R; m++) {
-        const int x = __shfl(d, (w->r0 + w0 + 16 * m + r) & 63, 64);
-        if (w0 + 16 * m + r < w->rows) depth[m] = x;
-      }
-      if (lane >= w->r0 && lane < nodes) deep = flat = d;
-    } else {
-      walk(parents, nodes, node);
-      for (int i = w->r0 + lane; i < nodes; i += 64) {
-        deep = max(deep, (int)node[i].y);
-        flat = min(flat, (int)node[i].y);
-      }
-#pragma unroll
-      for (int m = 0; m < R; m++)
-        if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
+    for (int i = w->r0 + lane; i < nodes; i += 64) {
+      deep = max(deep, (int)node[i].y);
+      flat = min(flat, (int)node[i].y);
     }
     w->deep = wave_extreme<true>(deep);
-    w->flat = wave_extreme<false>(flat);
+    w->windowed = w->deep - wave_extreme<false>(flat) < kWindow - kBlock;
   }
-  w->windowed = w->deep - w->flat < kWindow - kBlock;
 }
 
 // Q as the right operand: rows w0 + 16 m + r, features in the order of feature().
@@ -443,6 +467,8 @@ __device__ __forceinline__ u32x4 cut(u32x4 v, int left) {
 template <int DV, int R>
 __device__ __forceinline__ void put_part(const TreeArgs& a, const TreeSplit& sp, const Part& w,
                                          int w0, int head, const f32x4 (&acc)[R][DV / 16]) {
+  constexpr int NC = DV / 16;
+  typedef float fv __attribute__((ext_vector_type(NC < 4 ? NC : 4)));
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int64_t item = w.from / sp.chunk_len;
 #pragma unroll
@@ -452,10 +478,67 @@ __device__ __forceinline__ void put_part(const TreeArgs& a, const TreeSplit& sp,
       const int row = w0 + 16 * m + 4 * g + i;
       if (row >= w.rows) continue;
       float* dst = sp.part + ((item * a.ja.total_tokens + w.o + w.r0 + row) * a.ja.num_heads +
-                              head) * DV + r;
+                              head) * DV + NC * r;
 #pragma unroll
-      for (int c = 0; c < DV / 16; c++) dst[16 * c] = acc[m][c][i];
+      for (int c = 0; c < NC; c += 4) {
+        fv x;
+#pragma unroll
+        for (int e = 0; e < NC && e < 4; e++) x[e] = acc[m][c + e][i];
+        *reinterpret_cast<fv*>(dst + c) = x;
+      }
     }
+}
+
+// The outputs themselves, where all of a row's cached keys are summed up and no node
+// sees another one: with the row's own key.  The dot product is taken in the layout
+// of load_q (32 features a lane), the value row by row.
+template <int KIND, int DQK, int DV, int R>
+__device__ __forceinline__ void put_out(const TreeArgs& a, const Part& w, int w0, int head,
+                                        const bf16x8 (&q)[R][DQK / 32],
+                                        const f32x4 (&acc)[R][DV / 16]) {
+  constexpr int NC = DV / 16;
+  typedef __bf16 bv __attribute__((ext_vector_type(NC)));
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+  const int N = a.ja.max_seq_len;
+  const float bias = a.ja.rab_pos[N - 1] + a.ja.rab_time[0];  // of a token and itself
+  const float inv = 1.0f / (float)N;
+#pragma unroll
+  for (int m = 0; m < R; m++) {
+    const int own = min(w0 + 16 * m + r, w.rows - 1);
+    const uint16_t* kr =
+        (const uint16_t*)a.t.k + (w.o + w.r0 + own) * a.t.k_stride + (int64_t)head * DQK;
+    bv v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int64_t t = w.o + w.r0 + min(w0 + 16 * m + 4 * g + i, w.rows - 1);
+      v[i] = *reinterpret_cast<const bv*>((const uint16_t*)a.t.v + t * a.t.v_stride +
+                                          (int64_t)head * DV + NC * r);
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int st = 0; st < DQK / 32; st++) {
+      const bf16x8 k8 =
+          as_bf16x8(*reinterpret_cast<const u32x4*>(kr + feature<KIND, DQK>(st, g)));
+#pragma unroll
+      for (int e = 0; e < 8; e++) s = fmaf((float)q[m][st][e], (float)k8[e], s);
+    }
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    s += bias;
+    s *= sigmoid_fast(s);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float p = __shfl(s, 4 * g + i, 64);
+      const int row = w0 + 16 * m + 4 * g + i;
+      if (row >= w.rows) continue;
+      bv x;
+#pragma unroll
+      for (int c = 0; c < NC; c++)  // the weights' factor -log2(e) comes off
+        x[c] = (__bf16)(fmaf(p, (float)v[i][c], acc[m][c][i] * -0.6931471805599453f) * inv);
+      *reinterpret_cast<bv*>((uint16_t*)a.out +
+                             ((w.o + w.r0 + row) * a.ja.num_heads + head) * DV + NC * r) = x;
+    }
+  }
 }
 
 template <int KIND, int DQK, int DV, int R>
@@ -474,14 +557,55 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   __shared__ float sums[2 * 16 * R * DV];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Part w;
+  if (!find_place(a, sp, &w)) return;
+  const int first_page = fetch_page(a, w, w.from);
   if (!find_part(a, sp, &w)) return;
   const int lg = w.lg;
-  Ahead<4> h;
-  fetch<Q8>(a, w, w.from, fetch_page(a, w, w.from), &h);
   // A wave's head and share of the keys.
   const int ks_count = 4 / sp.hg, hh = wave % sp.hg, ks = wave / sp.hg;
   const int head = w.head0 + hh;
   const int r = lane % 16, g = lane / 16;
+  u32x4 kw[NT][(KW + 3) / 4];
+  u32x4 vw[NC];
+  // The loads of a tile: always the same number, of rows that exist, so that a
+  // wait for one of them waits for nothing behind it.
+  auto load_k = [&](int t0) {
+    const int at = t0 + GK * (r / 4);  // operand t takes row at + 4 t + r % 4
+    const char* src = (const char*)a.c.kc + (kb.rows16[at / 16] + ((int64_t)head << lg) +
+                                             at % 16 + r % 4) * (DQK * CB);
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      if constexpr (KW == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t * DQK * CB + 8 * g);
+        kw[t][0][0] = v.x;
+        kw[t][0][1] = v.y;
+      } else {
+#pragma unroll
+        for (int u = 0; u < KW / 4; u++)
+          kw[t][u] = *reinterpret_cast<const u32x4*>(src + 4 * t * DQK * CB + 64 * u + 16 * g);
+      }
+    }
+  };
+  auto load_v = [&](int t0) {
+    const int at = t0 + GK * g;
+    const int64_t row = kb.rows16[at / 16];
+    const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
+    const char* src =
+        (const char*)a.c.vc + (((((row >> lg) + head) * DV + NC * r) << lg) + place) * CB;
+#pragma unroll
+    for (int c = 0; c < NC; c++)
+      vw[c] = *reinterpret_cast<const u32x4*>(src + ((int64_t)(c * CB) << lg));
+  };
+  // The first tile is on its way before anything else is looked at.
+  put_rows(a, w, w.from, valid_page(a, w, w.from, first_page), &kb);
+  __syncthreads();
+  if (w.from + ks * T < w.to) {
+    load_k(ks * T);
+    load_v(ks * T);
+  }
+  Ahead<4> h;
+  fetch<Q8>(a, w, w.from, first_page, &h);
+  if (bound_depths(a, &w)) fetch_pos(a, w, w.from, &h);
   bf16x8 q[R][KS];
   load_q<KIND, DQK, R>(a, w, 0, head, q);
   f32x4 acc[R][NC];
@@ -492,52 +616,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   for (int i = tid; i < a.ja.num_buckets; i += kThreads)
     rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
   if (tid < 16 * R) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  const bool known = w.windowed;
   int depth[R];
   find_depths<R>(a, &w, 0, node, depth);
-  fetch_pos(a, w, w.from, &h);
+  if (!known) fetch_pos(a, w, w.from, &h);
+  __syncthreads();  // rs
 
-  u32x4 kw[NT][(KW + 3) / 4];
-  u32x4 vw[NC];
   for (int k0 = w.from; k0 < w.to; k0 += kBlock) {
     const int keys = min(kBlock, w.to - k0);
-    __syncthreads();  // the block before is done with what follows
-    put_rows(a, w, k0, h, &kb);
-    const int next_page = fetch_page(a, w, k0 + kBlock);
-    __syncthreads();
-    // The loads of a tile: always the same number, of rows that exist, so that a
-    // wait for one of them waits for nothing behind it.
-    auto load_k = [&](int t0) {
-      const int at = t0 + GK * (r / 4);  // operand t takes row at + 4 t + r % 4
-      const char* src = (const char*)a.c.kc + (kb.rows16[at / 16] + ((int64_t)head << lg) +
-                                               at % 16 + r % 4) * (DQK * CB);
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        if constexpr (KW == 2) {
-          const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t * DQK * CB + 8 * g);
-          kw[t][0][0] = v.x;
-          kw[t][0][1] = v.y;
-        } else {
-#pragma unroll
-          for (int u = 0; u < KW / 4; u++)
-            kw[t][u] = *reinterpret_cast<const u32x4*>(src + 4 * t * DQK * CB + 64 * u + 16 * g);
-        }
-      }
-    };
-    auto load_v = [&](int t0) {
-      const int at = t0 + GK * g;
-      const int64_t row = kb.rows16[at / 16];
-      const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
-      const char* src =
-          (const char*)a.c.vc + (((((row >> lg) + head) * DV + r) << lg) + place) * CB;
-#pragma unroll
-      for (int c = 0; c < NC; c++)
-        vw[c] = *reinterpret_cast<const u32x4*>(src + ((int64_t)(16 * c * CB) << lg));
-    };
     int t0 = ks * T;
-    if (t0 < keys) {
-      load_k(t0);
-      load_v(t0);
+    if (k0 != w.from) {
+      __syncthreads();  // the block before is done with what follows
+      put_rows(a, w, k0, h.page, &kb);
+      __syncthreads();
+      if (t0 < keys) {
+        load_k(t0);
+        load_v(t0);
+      }
     }
+    const int next_page = fetch_page(a, w, k0 + kBlock);
     put_keys<Q8>(a, w, rs, h, &kb);
     __syncthreads();
     if (k0 + kBlock < w.to) {
@@ -556,8 +653,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
 #pragma unroll
         for (int c = 0; c < NC; c++) vw[c] = cut<CB>(vw[c], left);
       }
+      f32x4 bias[NS][R][2];
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+        find_bias<4, R>(a, w, rs, kb, about, k0, t0 + GK * g + 8 * s, 0, depth, bias[s]);
 #pragma unroll
       for (int s = 0; s < NS; s++) {
+        const int at = t0 + GK * g + 8 * s;
         f32x4 sc[R][2];
 #pragma unroll
         for (int x = 0; x < 2; x++) {
@@ -576,9 +678,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
           }
         }
         if (s == NS - 1) load_k(next);
-        const int at = t0 + GK * g + 8 * s;
-        f32x4 bv[R][2], kf[2], vf[2];
-        find_bias<4, R>(a, w, rs, kb, about, k0, at, 0, depth, bv);
+        f32x4 kf[2], vf[2];
         if constexpr (Q8)
 #pragma unroll
           for (int x = 0; x < 2; x++) {
@@ -588,7 +688,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
         bf16x8 p[R];
 #pragma unroll
         for (int m = 0; m < R; m++)
-          p[m] = find_weights<Q8>(sc[m], bv[m], kf, vf, whole, left - 8 * s);
+          p[m] = find_weights<Q8>(sc[m], bias[s][m], kf, vf, whole, left - 8 * s);
 #pragma unroll
         for (int c = 0; c < NC; c++) {
           bf16x8 vf8;
@@ -602,11 +702,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
     }
   }
 
-  // The waves of a head add up, in order.
-  for (int x = 1; x < ks_count; x++) {
+  // The waves of a head add up: half of them to the other half, in order.
+  for (int half = ks_count / 2; half; half /= 2) {
     __syncthreads();
-    float* space = sums + hh * (16 * R * DV);
-    if (ks == x) {
+    float* space = sums + ((ks % half) * sp.hg + hh) * (16 * R * DV);
+    if (ks >= half && ks < 2 * half) {
 #pragma unroll
       for (int m = 0; m < R; m++)
 #pragma unroll
@@ -616,7 +716,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
             space[(16 * m + 4 * g + i) * DV + 16 * c + r] = acc[m][c][i];
     }
     __syncthreads();
-    if (ks == 0) {
+    if (ks < half) {
 #pragma unroll
       for (int m = 0; m < R; m++)
 #pragma unroll
@@ -626,7 +726,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
             acc[m][c][i] += space[(16 * m + 4 * g + i) * DV + 16 * c + r];
     }
   }
-  if (ks == 0) put_part<DV, R>(a, sp, w, 0, head, acc);
+  if (ks) return;
+  if (sp.last) put_out<KIND, DQK, DV, R>(a, w, 0, head, q, acc);
+  else put_part<DV, R>(a, sp, w, 0, head, acc);
 }
 
 // A tile of one head in LDS.  K: rows of keys, V: rows of features, in 16-byte
@@ -649,7 +751,10 @@ struct Tile {
     const int turn = (KP == 16 ? low | high << 2 : KP == 8 ? low | high << 1 : high) & (KP - 1);
     return (key * KP + (piece ^ turn)) * 16;
   }
-  __device__ static int v_at(int f, int piece) { return (f * 4 + (piece ^ (f >> 2 & 3))) * 16; }
+  // Column r of operand c; feature DV / 16 r + c.
+  __device__ static int v_at(int r, int c, int piece) {
+    return ((16 * c + r) * 4 + (piece ^ (r >> 2 & 3))) * 16;
+  }
 };
 
 template <int KIND, int DQK, int DV, int R>
@@ -662,15 +767,21 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   constexpr int KL = (Tl::kPieces + kThreads - 1) / kThreads;  // pieces a thread loads
   constexpr int VL = (Tl::vPieces + kThreads - 1) / kThreads;
   constexpr int TB = kBlock / T;                               // tiles of a block
+  // Tiles under way: two where the rows are few and the cache's bytes are the bound
+  // (a tile of 16 KB under way in each of two workgroups holds a CU to 4 TB/s).
+  constexpr int P = R == 1 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) Keys<1> kb[2];
   __shared__ __attribute__((aligned(16))) Tl tiles[2];
   __shared__ Rows rs;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Part w;
+  if (!find_place(a, sp, &w)) return;
+  const int first_page = fetch_page(a, w, w.from);
   if (!find_part(a, sp, &w)) return;
   const int lg = w.lg, head = w.head0;
   Ahead<1> h;
-  fetch<Q8>(a, w, w.from, fetch_page(a, w, w.from), &h);
+  fetch<Q8>(a, w, w.from, first_page, &h);
+  if (bound_depths(a, &w)) fetch_pos(a, w, w.from, &h);
   const int w0 = wave * 16 * R;  // the wave's first row within the workgroup's
   const bool idle = w0 >= w.rows;
   const int r = lane % 16, g = lane / 16;
@@ -684,30 +795,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   for (int i = tid; i < a.ja.num_buckets; i += kThreads)
     rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
   if (tid < kMaxRows) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
-  int depth[R];
-  static_assert(sizeof(tiles) >= kMaxDraft * sizeof(short2), "the depths fit where the tiles go");
-  find_depths<R>(a, &w, w0, reinterpret_cast<short2*>(tiles), depth);
-  fetch_pos(a, w, w.from, &h);
-  __syncthreads();
-  put_rows(a, w, w.from, h, &kb[0]);
-  put_keys<Q8>(a, w, rs, h, &kb[0]);
-  if (w.from + kBlock < w.to) {
-    fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
-    fetch_pos(a, w, w.from + kBlock, &h);
-  }
-  __syncthreads();
-
-  // Tile j of the chunk: loads into registers, then into LDS.
+  // Tile j of the chunk: loads into one of P sets of registers, then into LDS.
   const int count = (w.to - w.from + T - 1) / T;
-  u32x4 kr[KL], vr[VL];
-  auto load = [&](int j) {
+  u32x4 kr[P][KL], vr[P][VL];
+  auto load = [&](int j, int set) {
     const Keys<1>& k = kb[j / TB % 2];
     const int t0 = j % TB * T;
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads, at = t0 + x / KP;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      kr[e] = *reinterpret_cast<const u32x4*>(
+      kr[set][e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.kc +
           (k.rows16[at / 16] + ((int64_t)head << lg) + at % 16) * (DQK * CB) + x % KP * 16);
     }
@@ -717,7 +815,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
       const int64_t row = k.rows16[at / 16];
       const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
-      vr[e] = *reinterpret_cast<const u32x4*>(
+      vr[set][e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.vc + (((((row >> lg) + head) * DV + x / 4) << lg) + place) * CB);
     }
   };
@@ -726,38 +824,56 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
     const int about = __builtin_amdgcn_readfirstlane(kb[j / TB % 2].about[t0 / 64]);
     return (about & all) == all;
   };
-  auto store = [&](int j) {
+  auto store = [&](int j, int set) {
     Tl& tl = tiles[j % 2];
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[e];
+      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[set][e];
     }
     if (!is_whole(j)) {  // codes behind the last key count as zeros
       const Keys<1>& k = kb[j / TB % 2];
       const int at = j % TB * T + GK * (tid % 4);
       const int left = max(0, min(GK, k.left16[at / 16] - at % 16));
 #pragma unroll
-      for (int e = 0; e < VL; e++) vr[e] = cut<CB>(vr[e], left);
+      for (int e = 0; e < VL; e++) vr[set][e] = cut<CB>(vr[set][e], left);
     }
 #pragma unroll
     for (int e = 0; e < VL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
-      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4, x % 4)) = vr[e];
+      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4 / NC, x / 4 % NC, x % 4)) = vr[set][e];
     }
   };
-  load(0);
-  store(0);
+
+  int depth[R];
+  static_assert(sizeof(tiles) >= kMaxDraft * sizeof(short2), "the depths fit where the tiles go");
+  const bool known = w.windowed;
+  find_depths<R>(a, &w, w0, reinterpret_cast<short2*>(tiles), depth);
+  if (!known) fetch_pos(a, w, w.from, &h);
+  put_rows(a, w, w.from, h.page, &kb[0]);
   __syncthreads();
-  for (int j = 0; j < count; j++) {
-    const bool more = j + 1 < count;
-    if (more) load(j + 1);
-    // the next block's keys, two tiles before they are needed
+  if (count > 0) {
+    load(0, 0);
+    put_keys<Q8>(a, w, rs, h, &kb[0]);
+    if (w.from + kBlock < w.to) {
+      fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
+      fetch_pos(a, w, w.from + kBlock, &h);
+    }
+    __syncthreads();
+    store(0, 0);
+    if (P == 2 && count > 1) load(1, 1);
+    __syncthreads();
+  }
+  auto turn = [&](int j, auto odd) {
+    // P tiles ahead, in the registers of the tile that is in LDS by now
+    constexpr int set = P == 2 ? decltype(odd)::value : 0;
+    if (j + P < count) load(j + P, set);
+    // the next block's keys, before their first tile's loads
     const int k1 = w.from + (j / TB + 1) * kBlock;
-    if (j % TB == TB - 3 && k1 < w.to) {
-      put_rows(a, w, k1, h, &kb[(j / TB + 1) % 2]);
+    if (j % TB == TB - P - 2 && k1 < w.to) {
+      put_rows(a, w, k1, h.page, &kb[(j / TB + 1) % 2]);
       put_keys<Q8>(a, w, rs, h, &kb[(j / TB + 1) % 2]);
       if (k1 + kBlock < w.to) {
         fetch<Q8>(a, w, k1 + kBlock, fetch_page(a, w, k1 + kBlock), &h);
@@ -775,8 +891,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
         const int at = t0 + GK * g;
         left = max(0, min(GK, k.left16[at / 16] - at % 16));
       }
+      f32x4 bias[NS][R][2];
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+        find_bias<1, R>(a, w, rs, k, about, k0, t0 + GK * g + 8 * s, w0, depth, bias[s]);
 #pragma unroll
       for (int s = 0; s < NS; s++) {
+        const int at = t0 + GK * g + 8 * s;
         f32x4 sc[R][2];
 #pragma unroll
         for (int x = 0; x < 2; x++) {
@@ -804,9 +925,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
             }
           }
         }
-        const int at = t0 + GK * g + 8 * s;
-        f32x4 bv[R][2], kf[2], vf[2];
-        find_bias<1, R>(a, w, rs, k, about, k0, at, w0, depth, bv);
+        f32x4 kf[2], vf[2];
         if constexpr (Q8)
 #pragma unroll
           for (int x = 0; x < 2; x++) {
@@ -816,11 +935,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
         bf16x8 p[R];
 #pragma unroll
         for (int m = 0; m < R; m++)
-          p[m] = find_weights<Q8>(sc[m], bv[m], kf, vf, whole, left - 8 * s);
+          p[m] = find_weights<Q8>(sc[m], bias[s][m], kf, vf, whole, left - 8 * s);
 #pragma unroll
         for (int c = 0; c < NC; c++) {
           bf16x8 v8;
-          const char* src = tl.v + Tl::v_at(16 * c + r, g);
+          const char* src = tl.v + Tl::v_at(r, c, g);
           if constexpr (Q8) {
             const uint2 x = *reinterpret_cast<const uint2*>(src + 8 * s);
             v8 = widen<KIND>(x.x, x.y);
@@ -832,10 +951,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
         }
       }
     }
-    if (more) store(j + 1);
+    if (j + 1 < count) store(j + 1, P == 2 ? 1 - set : 0);
     __syncthreads();
+  };
+  for (int j = 0; j < count; j += 2) {
+    turn(j, std::integral_constant<int, 0>{});
+    if (j + 1 < count) turn(j + 1, std::integral_constant<int, 1>{});
   }
-  if (!idle) put_part<DV, R>(a, sp, w, w0, head, acc);
+  if (idle) return;
+  if (sp.last) put_out<KIND, DQK, DV, R>(a, w, w0, head, q, acc);
+  else put_part<DV, R>(a, sp, w, w0, head, acc);
 }
 
 // The launch for one kind of cache.

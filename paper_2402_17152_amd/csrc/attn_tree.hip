@@ -270,7 +270,7 @@ hipError_t launch_attn_tree(const TreeArgs& a, const TreeSplit& sp, int kind, hi
   hipError_t e = kind == kCacheBf16   ? tree::launch_bf16(a, sp, s)
                  : kind == kCacheE4m3 ? tree::launch_e4m3(a, sp, s)
                                       : tree::launch_int8(a, sp, s);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || sp.last) return e;
   // Rows of a workgroup: one, while there are few of them.
   const int waves = sp.chunks > 16 ? 4 : 1;
   const int64_t T = a.ja.total_tokens;

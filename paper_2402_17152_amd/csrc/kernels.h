@@ -336,6 +336,7 @@ struct TreeSplit {
   int32_t hg;         // heads a workgroup takes: 1, 2 or 4
   int32_t rows;       // drafted rows it takes
   int32_t row_blocks;
+  int32_t last;       // outputs, not partial ones: one chunk, and no node sees another
 };
 // The split for these sizes, part left null.
 TreeSplit tree_split(int32_t num_seqs, int64_t total_tokens, int32_t num_heads, int32_t max_seq_len,
