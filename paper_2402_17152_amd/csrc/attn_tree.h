@@ -45,29 +45,31 @@ namespace tree {
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;       // keys whose scales, times and pages are held
 constexpr int kWindow = 512;      // entries of rab_pos that are held
-constexpr int kMaxRows = 128;     // drafted rows of a workgroup
 constexpr float kNegLog2e = -kLog2e;
 
 // What is known of 64 keys: each row's time bucket is the same for all; the time
 // differences fit 32 bits; all of the first, the second 32 keys are there.
 enum { kOneBucket = 1, kNear = 2, kWhole = 4 };
 
-// What the waves of a workgroup know of kBlock keys; HG: heads.
-template <int HG>
+// What the waves of a workgroup know of kBlock keys; HG: heads, ROWS: drafted rows.
+template <int HG, int ROWS>
 struct Keys {
+  static constexpr int heads = HG;
   float scales[2][HG][kBlock];     // k (times -log2(e)) and v
   float window[4][kWindow + 8];    // part of rab_pos (times -log2(e)), four shifted copies
   int64_t time[kBlock];
+  int time32[kBlock];              // its low word
   int64_t rows16[kBlock / 16];     // first cache row of 16 keys for head 0
   int left16[kBlock / 16];         // how many of them are there; of none, row 0 is read
-  float uniform[4][kMaxRows];      // the rows' entry of rtime for 64 keys (kOneBucket)
+  float uniform[4][ROWS];          // the rows' entry of rtime for 64 keys (kOneBucket)
   int about[4];                    // what is known of 64 keys
 };
 
 // What they know of the drafted rows.
+template <int ROWS>
 struct Rows {
   float rtime[256];                // rab_time, times -log2(e)
-  int64_t time[kMaxRows];
+  int64_t time[ROWS];
 };
 
 // Two words of codes (8 of them) as bf16.
@@ -266,9 +268,9 @@ __device__ __forceinline__ void fetch_pos(const TreeArgs& a, const Part& w, int 
 }
 
 // Where the rows of a block's keys are.
-template <int HG>
-__device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k0,
-                                         int64_t page, Keys<HG>* k) {
+template <typename K>
+__device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k0, int64_t page,
+                                         K* k) {
   const uint64_t there = __ballot(page >= 0);
   const int tid = threadIdx.x;
   if (tid % 16 == 0) {
@@ -280,11 +282,12 @@ __device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k
 }
 
 // The rest of what is known of them.
-template <bool Q8, int HG>
-__device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const Rows& rows,
-                                         const Ahead<HG>& h, Keys<HG>* k) {
+template <bool Q8, int HG, int ROWS>
+__device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const Rows<ROWS>& rows,
+                                         const Ahead<HG>& h, Keys<HG, ROWS>* k) {
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   k->time[tid] = h.time;
+  k->time32[tid] = (int)h.time;
   if constexpr (Q8)
 #pragma unroll
     for (int x = 0; x < HG; x++)
@@ -333,19 +336,17 @@ __device__ __forceinline__ bool bound_depths(const TreeArgs& a, Part* w) {
 }
 
 // Depths of this lane's rows w0 + 16 m + r (0 where there is none), and, where
-// bound_depths() does not know them, the window's.
+// bound_depths() does not know them, the window's.  parent: of node `lane`.
 template <int R>
-__device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, short2* node,
-                                            int* depth) {
+__device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, int64_t parent,
+                                            short2* node, int* depth) {
   const int lane = threadIdx.x % 64, r = lane % 16;
   const int nodes = w->r0 + w->rows;
 #pragma unroll
   for (int m = 0; m < R; m++) depth[m] = 0;
   if (!a.parents) return;
-  const int64_t* parents = a.parents + w->o;
   if (nodes <= 64) {
-    const int64_t p = lane < nodes ? parents[lane] : -1;
-    const int d = walk64(p >= 0 && p < lane ? (int)p : -1);
+    const int d = walk64(parent >= 0 && parent < lane ? (int)parent : -1);
 #pragma unroll
     for (int m = 0; m < R; m++) {
       const int x = __shfl(d, (w->r0 + w0 + 16 * m + r) & 63, 64);
@@ -357,7 +358,7 @@ __device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, 
     }
     return;
   }
-  walk(parents, nodes, node);
+  walk(a.parents + w->o, nodes, node);
 #pragma unroll
   for (int m = 0; m < R; m++)
     if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
@@ -392,9 +393,9 @@ __device__ __forceinline__ void load_q(const TreeArgs& a, const Part& w, int w0,
 }
 
 // -log2(e) times the bias of this lane's rows and the eight keys k0 + at ..
-template <int HG, int R>
-__device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, const Rows& rows,
-                                          const Keys<HG>& k, int about, int k0, int at, int w0,
+template <int R, int HG, int ROWS>
+__device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, const Rows<ROWS>& rows,
+                                          const Keys<HG, ROWS>& k, int about, int k0, int at, int w0,
                                           const int* depth, f32x4 (&bv)[R][2]) {
   const int r = threadIdx.x % 16;
   if (w.windowed && (about & kOneBucket)) {
@@ -413,21 +414,33 @@ __device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, cons
   for (int m = 0; m < R; m++) {
     const int64_t rt = rows.time[w0 + 16 * m + r];
     const int shift = max(0, min(w.deep - depth[m], kWindow - kBlock - 1));
+    int bucket[8];
+    if (about & kNear) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const int far = N - 1 + k0 + at + i - w.n_b - depth[m];
-      const float pos =
-          w.windowed ? k.window[0][shift + at + i] : a.ja.rab_pos[max(0, far)] * kNegLog2e;
-      const int64_t kt = k.time[at + i];
-      int bucket;
-      if (about & kNear) {
-        const int dt = (int)rt - (int)kt;
-        bucket = min(31 - __clz(max(1, max(dt, -dt))), a.ja.num_buckets - 1);
-      } else {
-        bucket = time_bucket64(rt - kt, a.ja.num_buckets);
+      for (int i = 0; i < 8; i++) {
+        const int dt = (int)rt - k.time32[at + i];
+        bucket[i] = min(31 - __clz(max(1, max(dt, -dt))), a.ja.num_buckets - 1);
       }
-      bv[m][i / 4][i % 4] = pos + rows.rtime[bucket];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) bucket[i] = time_bucket64(rt - k.time[at + i], a.ja.num_buckets);
     }
+    float pos[8];
+    if (w.windowed) {
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const f32x4 v =
+            *reinterpret_cast<const f32x4*>(&k.window[shift & 3][(shift & ~3) + at + 4 * x]);
+#pragma unroll
+        for (int i = 0; i < 4; i++) pos[4 * x + i] = v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        pos[i] = a.ja.rab_pos[max(0, N - 1 + k0 + at + i - w.n_b - depth[m])] * kNegLog2e;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) bv[m][i / 4][i % 4] = pos[i] + rows.rtime[bucket[i]];
   }
 }
 
@@ -541,7 +554,8 @@ __device__ __forceinline__ void put_out(const TreeArgs& a, const Part& w, int w0
   }
 }
 
-template <int KIND, int DQK, int DV, int R>
+// H4: the four waves have a head each, else they share heads and keys as sp.hg says.
+template <int KIND, int DQK, int DV, int R, bool H4>
 __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeArgs a,
                                                                     const TreeSplit sp) {
   constexpr bool Q8 = KIND != kCacheBf16;     // quantised
@@ -551,161 +565,189 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   constexpr int NT = T / 16, NS = T / 32;     // operands of K, contraction steps of P V
   constexpr int KW = DQK * CB / 16;           // words of a K row a lane reads
   constexpr int KS = DQK / 32, NC = DV / 16;  // contraction steps of K Q^T, column tiles
-  __shared__ __attribute__((aligned(16))) Keys<4> kb;
-  __shared__ Rows rs;
-  __shared__ short2 node[kMaxDraft];
-  __shared__ float sums[2 * 16 * R * DV];
+  // Tiles a wave has under way: the compute units' share of the memory's latency is
+  // 43 KB; two tiles where the registers hold them.
+  constexpr int P = H4 && R == 1 && DQK + DV <= 128 ? 2 : 1;
+  using Kb = Keys<4, 16 * R>;
+  __shared__ __attribute__((aligned(16))) union {
+    Kb kb[2];
+    float sums[2 * 16 * R * DV];
+    struct {
+      Kb first;
+      short2 node[kMaxDraft];
+    };
+  } sh;
+  static_assert(sizeof(Kb) >= sizeof(sh.node), "the depths fit where the second block goes");
+  __shared__ Rows<16 * R> rs;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Part w;
   if (!find_place(a, sp, &w)) return;
   const int first_page = fetch_page(a, w, w.from);
   if (!find_part(a, sp, &w)) return;
   const int lg = w.lg;
-  // A wave's head and share of the keys.
-  const int ks_count = 4 / sp.hg, hh = wave % sp.hg, ks = wave / sp.hg;
+  // A wave's head and share of the keys: tile j is tile j % turns of its share of
+  // block j / turns.
+  const int hg = H4 ? 4 : sp.hg, ks_count = 4 / hg, hh = wave % hg, ks = wave / hg;
+  const int turns = kBlock / T / ks_count;
   const int head = w.head0 + hh;
   const int r = lane % 16, g = lane / 16;
-  u32x4 kw[NT][(KW + 3) / 4];
-  u32x4 vw[NC];
+  u32x4 kw[P][NT][(KW + 3) / 4];
+  u32x4 vw[P][NC];
   // The loads of a tile: always the same number, of rows that exist, so that a
   // wait for one of them waits for nothing behind it.
-  auto load_k = [&](int t0) {
-    const int at = t0 + GK * (r / 4);  // operand t takes row at + 4 t + r % 4
-    const char* src = (const char*)a.c.kc + (kb.rows16[at / 16] + ((int64_t)head << lg) +
-                                             at % 16 + r % 4) * (DQK * CB);
+  auto load_k = [&](int j, int set) {
+    // operand t takes row at + 4 t + r % 4
+    const int at = (j % turns * ks_count + ks) * T + GK * (r / 4);
+    const char* src = (const char*)a.c.kc + (sh.kb[j / turns % 2].rows16[at / 16] +
+                                             ((int64_t)head << lg) + at % 16 + r % 4) * (DQK * CB);
 #pragma unroll
     for (int t = 0; t < NT; t++) {
       if constexpr (KW == 2) {
         const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t * DQK * CB + 8 * g);
-        kw[t][0][0] = v.x;
-        kw[t][0][1] = v.y;
+        kw[set][t][0][0] = v.x;
+        kw[set][t][0][1] = v.y;
       } else {
 #pragma unroll
         for (int u = 0; u < KW / 4; u++)
-          kw[t][u] = *reinterpret_cast<const u32x4*>(src + 4 * t * DQK * CB + 64 * u + 16 * g);
+          kw[set][t][u] =
+              *reinterpret_cast<const u32x4*>(src + 4 * t * DQK * CB + 64 * u + 16 * g);
       }
     }
   };
-  auto load_v = [&](int t0) {
-    const int at = t0 + GK * g;
-    const int64_t row = kb.rows16[at / 16];
+  auto load_v = [&](int j, int set) {
+    const int at = (j % turns * ks_count + ks) * T + GK * g;
+    const int64_t row = sh.kb[j / turns % 2].rows16[at / 16];
     const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
     const char* src =
         (const char*)a.c.vc + (((((row >> lg) + head) * DV + NC * r) << lg) + place) * CB;
 #pragma unroll
     for (int c = 0; c < NC; c++)
-      vw[c] = *reinterpret_cast<const u32x4*>(src + ((int64_t)(c * CB) << lg));
+      vw[set][c] = *reinterpret_cast<const u32x4*>(src + ((int64_t)(c * CB) << lg));
   };
-  // The first tile is on its way before anything else is looked at.
-  put_rows(a, w, w.from, valid_page(a, w, w.from, first_page), &kb);
-  __syncthreads();
-  if (w.from + ks * T < w.to) {
-    load_k(ks * T);
-    load_v(ks * T);
-  }
+  // What the workgroup needs once is asked for first, then the first tiles: loads
+  // come back in order, and the few small ones should not wait for the many.
   Ahead<4> h;
   fetch<Q8>(a, w, w.from, first_page, &h);
   if (bound_depths(a, &w)) fetch_pos(a, w, w.from, &h);
   bf16x8 q[R][KS];
   load_q<KIND, DQK, R>(a, w, 0, head, q);
+  const float bucket_bias = tid < a.ja.num_buckets ? a.ja.rab_time[tid] : 0.0f;
+  const int64_t row_time = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  const int64_t parent = a.parents && lane < w.r0 + w.rows ? a.parents[w.o + lane] : -1;
+  put_rows(a, w, w.from, h.page, &sh.kb[0]);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < P; j++) {
+    load_k(j, j);
+    load_v(j, j);
+  }
   f32x4 acc[R][NC];
 #pragma unroll
   for (int m = 0; m < R; m++)
 #pragma unroll
     for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = tid; i < a.ja.num_buckets; i += kThreads)
-    rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
-  if (tid < 16 * R) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  rs.rtime[tid] = bucket_bias * kNegLog2e;
+  if (tid < 16 * R) rs.time[tid] = row_time;
   const bool known = w.windowed;
   int depth[R];
-  find_depths<R>(a, &w, 0, node, depth);
+  find_depths<R>(a, &w, 0, parent, sh.node, depth);
   if (!known) fetch_pos(a, w, w.from, &h);
   __syncthreads();  // rs
+  put_keys<Q8>(a, w, rs, h, &sh.kb[0]);
+  if (w.from + kBlock < w.to) {
+    fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
+    fetch_pos(a, w, w.from + kBlock, &h);
+  }
+  __syncthreads();
 
-  for (int k0 = w.from; k0 < w.to; k0 += kBlock) {
-    const int keys = min(kBlock, w.to - k0);
-    int t0 = ks * T;
-    if (k0 != w.from) {
-      __syncthreads();  // the block before is done with what follows
-      put_rows(a, w, k0, h.page, &kb);
-      __syncthreads();
-      if (t0 < keys) {
-        load_k(t0);
-        load_v(t0);
-      }
+  auto tile = [&](int j, int k0, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    const Kb& kb = sh.kb[j / turns % 2];
+    const int t0 = (j % turns * ks_count + ks) * T;
+    const int about = __builtin_amdgcn_readfirstlane(kb.about[t0 / 64]);
+    const int all = Q8 ? 3 * kWhole : kWhole << (t0 / 32 % 2);
+    const bool whole = (about & all) == all;  // all keys are there
+    // the last loads are of a block that has not been looked at: not used
+    const int next = min(j + P, (w.to - w.from + kBlock - 1) / kBlock * turns - 1);
+    int left = GK;                            // keys of this lane's group
+    if (!whole) {
+      const int at = t0 + GK * g;
+      left = max(0, min(GK, kb.left16[at / 16] - at % 16));
+#pragma unroll
+      for (int c = 0; c < NC; c++) vw[set][c] = cut<CB>(vw[set][c], left);
     }
-    const int next_page = fetch_page(a, w, k0 + kBlock);
-    put_keys<Q8>(a, w, rs, h, &kb);
-    __syncthreads();
-    if (k0 + kBlock < w.to) {
-      fetch<Q8>(a, w, k0 + kBlock, next_page, &h);
-      fetch_pos(a, w, k0 + kBlock, &h);
-    }
-    for (; t0 < keys; t0 += ks_count * T) {
-      const int next = min(t0 + ks_count * T, kBlock - T);  // a tile too many is not used
-      const int about = __builtin_amdgcn_readfirstlane(kb.about[t0 / 64]);
-      const int all = Q8 ? 3 * kWhole : kWhole << (t0 / 32 % 2);
-      const bool whole = (about & all) == all;  // all keys are there
-      int left = GK;                            // keys of this lane's group
-      if (!whole) {
-        const int at = t0 + GK * g;
-        left = max(0, min(GK, kb.left16[at / 16] - at % 16));
+    f32x4 bias[NS][R][2];
 #pragma unroll
-        for (int c = 0; c < NC; c++) vw[c] = cut<CB>(vw[c], left);
+    for (int s = 0; s < NS; s++)
+      find_bias<R>(a, w, rs, kb, about, k0, t0 + GK * g + 8 * s, 0, depth, bias[s]);
+#pragma unroll
+    for (int s = 0; s < NS; s++) {
+      const int at = t0 + GK * g + 8 * s;
+      f32x4 sc[R][2];
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const int t = 2 * s + x;
+#pragma unroll
+        for (int m = 0; m < R; m++) sc[m][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int st = 0; st < KS; st++) {
+          bf16x8 kf;
+          if constexpr (Q8)
+            kf = widen<KIND>(kw[set][t][st / 2][st % 2 * 2], kw[set][t][st / 2][st % 2 * 2 + 1]);
+          else
+            kf = as_bf16x8(kw[set][t][st]);
+#pragma unroll
+          for (int m = 0; m < R; m++) sc[m][x] = mfma16x16x32(kf, q[m][st], sc[m][x]);
+        }
       }
-      f32x4 bias[NS][R][2];
-#pragma unroll
-      for (int s = 0; s < NS; s++)
-        find_bias<4, R>(a, w, rs, kb, about, k0, t0 + GK * g + 8 * s, 0, depth, bias[s]);
-#pragma unroll
-      for (int s = 0; s < NS; s++) {
-        const int at = t0 + GK * g + 8 * s;
-        f32x4 sc[R][2];
+      if (s == NS - 1) load_k(next, set);
+      f32x4 kf[2], vf[2];
+      if constexpr (Q8)
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const int t = 2 * s + x;
-#pragma unroll
-          for (int m = 0; m < R; m++) sc[m][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int st = 0; st < KS; st++) {
-            bf16x8 kf;
-            if constexpr (Q8)
-              kf = widen<KIND>(kw[t][st / 2][st % 2 * 2], kw[t][st / 2][st % 2 * 2 + 1]);
-            else
-              kf = as_bf16x8(kw[t][st]);
-#pragma unroll
-            for (int m = 0; m < R; m++) sc[m][x] = mfma16x16x32(kf, q[m][st], sc[m][x]);
-          }
+          kf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[0][hh][at + 4 * x]);
+          vf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[1][hh][at + 4 * x]);
         }
-        if (s == NS - 1) load_k(next);
-        f32x4 kf[2], vf[2];
-        if constexpr (Q8)
+      bf16x8 p[R];
 #pragma unroll
-          for (int x = 0; x < 2; x++) {
-            kf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[0][hh][at + 4 * x]);
-            vf[x] = *reinterpret_cast<const f32x4*>(&kb.scales[1][hh][at + 4 * x]);
-          }
-        bf16x8 p[R];
+      for (int m = 0; m < R; m++)
+        p[m] = find_weights<Q8>(sc[m], bias[s][m], kf, vf, whole, left - 8 * s);
 #pragma unroll
-        for (int m = 0; m < R; m++)
-          p[m] = find_weights<Q8>(sc[m], bias[s][m], kf, vf, whole, left - 8 * s);
+      for (int c = 0; c < NC; c++) {
+        bf16x8 vf8;
+        if constexpr (Q8) vf8 = widen<KIND>(vw[set][c][2 * s], vw[set][c][2 * s + 1]);
+        else vf8 = as_bf16x8(vw[set][c]);
 #pragma unroll
-        for (int c = 0; c < NC; c++) {
-          bf16x8 vf8;
-          if constexpr (Q8) vf8 = widen<KIND>(vw[c][2 * s], vw[c][2 * s + 1]);
-          else vf8 = as_bf16x8(vw[c]);
-#pragma unroll
-          for (int m = 0; m < R; m++) acc[m][c] = mfma16x16x32(p[m], vf8, acc[m][c]);
+        for (int m = 0; m < R; m++) acc[m][c] = mfma16x16x32(p[m], vf8, acc[m][c]);
+      }
+    }
+    load_v(next, set);
+  };
+  for (int n = 0, k0 = w.from; k0 < w.to; n++, k0 += kBlock) {
+    const int keys = min(kBlock, w.to - k0), k1 = k0 + kBlock;
+    for (int i = 0; i < turns; i += P) {
+      if (i == turns - P && k1 < w.to) {
+        // the next block, before the first loads of its tiles
+        __syncthreads();  // the block before is done with
+        put_rows(a, w, k1, h.page, &sh.kb[(n + 1) % 2]);
+        put_keys<Q8>(a, w, rs, h, &sh.kb[(n + 1) % 2]);
+        __syncthreads();
+        if (k1 + kBlock < w.to) {
+          fetch<Q8>(a, w, k1 + kBlock, fetch_page(a, w, k1 + kBlock), &h);
+          fetch_pos(a, w, k1 + kBlock, &h);
         }
       }
-      load_v(next);
+      if ((i * ks_count + ks) * T >= keys) break;
+      tile(n * turns + i, k0, std::integral_constant<int, 0>{});
+      if constexpr (P == 2)
+        if ((i + 1) * T < keys) tile(n * turns + i + 1, k0, std::integral_constant<int, 1>{});
     }
   }
 
   // The waves of a head add up: half of them to the other half, in order.
   for (int half = ks_count / 2; half; half /= 2) {
     __syncthreads();
-    float* space = sums + ((ks % half) * sp.hg + hh) * (16 * R * DV);
+    float* space = sh.sums + ((ks % half) * hg + hh) * (16 * R * DV);
     if (ks >= half && ks < 2 * half) {
 #pragma unroll
       for (int m = 0; m < R; m++)
@@ -770,9 +812,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   // Tiles under way: two where the rows are few and the cache's bytes are the bound
   // (a tile of 16 KB under way in each of two workgroups holds a CU to 4 TB/s).
   constexpr int P = R == 1 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) Keys<1> kb[2];
+  using Kb = Keys<1, 64 * R>;
+  __shared__ __attribute__((aligned(16))) Kb kb[2];
   __shared__ __attribute__((aligned(16))) Tl tiles[2];
-  __shared__ Rows rs;
+  __shared__ Rows<64 * R> rs;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Part w;
   if (!find_place(a, sp, &w)) return;
@@ -792,14 +835,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   for (int m = 0; m < R; m++)
 #pragma unroll
     for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = tid; i < a.ja.num_buckets; i += kThreads)
-    rs.rtime[i] = a.ja.rab_time[i] * kNegLog2e;
-  if (tid < kMaxRows) rs.time[tid] = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  const float bucket_bias = tid < a.ja.num_buckets ? a.ja.rab_time[tid] : 0.0f;
+  const int64_t row_time = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
+  const int64_t parent = a.parents && lane < w.r0 + w.rows ? a.parents[w.o + lane] : -1;
+  rs.rtime[tid] = bucket_bias * kNegLog2e;
+  if (tid < 64 * R) rs.time[tid] = row_time;
   // Tile j of the chunk: loads into one of P sets of registers, then into LDS.
   const int count = (w.to - w.from + T - 1) / T;
   u32x4 kr[P][KL], vr[P][VL];
   auto load = [&](int j, int set) {
-    const Keys<1>& k = kb[j / TB % 2];
+    const Kb& k = kb[j / TB % 2];
     const int t0 = j % TB * T;
 #pragma unroll
     for (int e = 0; e < KL; e++) {
@@ -833,7 +878,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
       *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[set][e];
     }
     if (!is_whole(j)) {  // codes behind the last key count as zeros
-      const Keys<1>& k = kb[j / TB % 2];
+      const Kb& k = kb[j / TB % 2];
       const int at = j % TB * T + GK * (tid % 4);
       const int left = max(0, min(GK, k.left16[at / 16] - at % 16));
 #pragma unroll
@@ -850,7 +895,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   int depth[R];
   static_assert(sizeof(tiles) >= kMaxDraft * sizeof(short2), "the depths fit where the tiles go");
   const bool known = w.windowed;
-  find_depths<R>(a, &w, w0, reinterpret_cast<short2*>(tiles), depth);
+  find_depths<R>(a, &w, w0, parent, reinterpret_cast<short2*>(tiles), depth);
   if (!known) fetch_pos(a, w, w.from, &h);
   put_rows(a, w, w.from, h.page, &kb[0]);
   __syncthreads();
@@ -881,7 +926,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
       }
     }
     if (!idle) {
-      const Keys<1>& k = kb[j / TB % 2];
+      const Kb& k = kb[j / TB % 2];
       const Tl& tl = tiles[j % 2];
       const int t0 = j % TB * T, k0 = w.from + j / TB * kBlock;
       const int about = __builtin_amdgcn_readfirstlane(k.about[t0 / 64]);
@@ -894,7 +939,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
       f32x4 bias[NS][R][2];
 #pragma unroll
       for (int s = 0; s < NS; s++)
-        find_bias<1, R>(a, w, rs, k, about, k0, t0 + GK * g + 8 * s, w0, depth, bias[s]);
+        find_bias<R>(a, w, rs, k, about, k0, t0 + GK * g + 8 * s, w0, depth, bias[s]);
 #pragma unroll
       for (int s = 0; s < NS; s++) {
         const int at = t0 + GK * g + 8 * s;
@@ -973,8 +1018,12 @@ hipError_t launch(const TreeArgs& a, const TreeSplit& sp, hipStream_t s) {
     return hipGetLastError();
   };
 #define HSTU_TREE_R(DQK, DV)                                             \
-  if (sp.rows == 16) return go(attn_tree_few_kernel<KIND, DQK, DV, 1>);  \
-  if (sp.rows == 32) return go(attn_tree_few_kernel<KIND, DQK, DV, 2>);  \
+  if (sp.rows == 16)                                                     \
+    return sp.hg == 4 ? go(attn_tree_few_kernel<KIND, DQK, DV, 1, true>)  \
+                      : go(attn_tree_few_kernel<KIND, DQK, DV, 1, false>); \
+  if (sp.rows == 32)                                                     \
+    return sp.hg == 4 ? go(attn_tree_few_kernel<KIND, DQK, DV, 2, true>)  \
+                      : go(attn_tree_few_kernel<KIND, DQK, DV, 2, false>); \
   if (sp.rows == 64) return go(attn_tree_many_kernel<KIND, DQK, DV, 1>); \
   return go(attn_tree_many_kernel<KIND, DQK, DV, 2>);
 #define HSTU_TREE_DV(DQK)                       \
