@@ -605,7 +605,7 @@ def _rows(name, t, shape, dtype):
 
 def _dense_out(name, out, like, shape, dtype):
     if out is None:
-        return like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape) if like.dtype == dtype else like.new_empty(shape, dtype=dtype)
     if out.dtype != dtype or out.shape != torch.Size(shape) or not out.is_contiguous():
         raise ValueError(f"{name} must be contiguous {tuple(shape)} of {dtype}")
     return out
@@ -615,7 +615,7 @@ def _on_device(*tensors):
     """The launches go to the current device: every array has to lie there."""
     device = _raw_device() if _raw_device is not None else torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != device):
+        if t is not None and t.get_device() != device:  # -1 on the CPU
             raise ValueError(f"an array is on {t.device}, the current device is cuda:{device}")
 
 
@@ -640,7 +640,8 @@ def _rotary(call, q, k, inv_freq, seq_offsets, num_targets, positions, interleav
     shape, dtype = one.shape, one.dtype
     T, H, d = shape
     code = _dtype_code(one)
-    qs, ks = (0 if t is None else _rows(n, t, shape, dtype) for n, t in (("q", q), ("k", k)))
+    qs = 0 if q is None else _rows("q", q, shape, dtype)
+    ks = 0 if k is None else _rows("k", k, shape, dtype)
     freq = _array("inv_freq", inv_freq, torch.float64)
     pos = _array("positions", positions, torch.int64, T)
     offs, B = (None, 1) if seq_offsets is None else _offsets(seq_offsets)
@@ -708,6 +709,10 @@ class PagedCache:
         if k_scale is not None and (k_scale.shape != (pages, heads, page)
                                     or v_scale.shape != (pages, heads, page)):
             raise ValueError(f"scales must be {(pages, heads, page)}")
+        device = k.get_device()
+        for t in (v, timestamps, page_table, lengths, k_scale, v_scale):
+            if t is not None and t.get_device() != device:
+                raise ValueError(f"the cache's arrays are on {k.device} and {t.device}")
         self._arrays = (k, v, timestamps, page_table, lengths, k_scale, v_scale)
         self._shape = (B, heads, d_qk, d_v)
         self._desc = CacheDesc(pages, page, width, kind, _array("k", k, k.dtype),
@@ -757,7 +762,7 @@ def hstu_cache_write(k, v, timestamps, seq_offsets, cache, starts=None, stream=N
     vs = _rows("v", v, (T, H, dv), k.dtype)
     ts = _array("timestamps", timestamps, torch.int64, T)
     st = _array("starts", starts, torch.int64, B)
-    _on_device(k, v, timestamps, seq_offsets, starts, *cache._arrays)
+    _on_device(k, v, timestamps, seq_offsets, starts, cache.k)
     p = Problem(B, T, 1, H, dqk, dv, 1, code)
     _check(lib.hstu_cache_write(ctypes.byref(p), ctypes.byref(cache._desc), offs, st, ts, _ptr(k),
                                 ks, _ptr(v), vs, _stream(stream)))
@@ -777,7 +782,7 @@ def hstu_cache_read(cache, seq_offsets, total_tokens, starts=None, dtype=torch.b
     k = _dense_out("k", k, cache.k, (T, H, dqk), dtype)
     v = _dense_out("v", v, cache.k, (T, H, dv), dtype)
     ts = _dense_out("timestamps", ts, cache.k, (T,), torch.int64)
-    _on_device(seq_offsets, starts, k, v, ts, *cache._arrays)
+    _on_device(seq_offsets, starts, k, v, ts, cache.k)
     p = Problem(B, T, 1, H, dqk, dv, 1, _dtype_code(k))
     _check(lib.hstu_cache_read(ctypes.byref(p), ctypes.byref(cache._desc), offs, st, _ptr(k),
                                _ptr(v), _ptr(ts), _stream(stream)))
@@ -787,7 +792,7 @@ def hstu_cache_read(cache, seq_offsets, total_tokens, starts=None, dtype=torch.b
 def hstu_cache_validate(cache, stream=None):
     """Raises HstuError where lengths or the page table lead out of the pool."""
     B, H, dqk, dv = cache._shape
-    _on_device(*cache._arrays)
+    _on_device(cache.k)
     p = Problem(B, 0, 1, H, dqk, dv, 1, HSTU_BF16)
     _check(lib.hstu_cache_validate(ctypes.byref(p), ctypes.byref(cache._desc), _stream(stream)))
 
@@ -822,9 +827,8 @@ def hstu_attn_fwd_tree(q, k, v, seq_offsets, timestamps, cache, rab_pos, rab_tim
     p = Problem(B, T, max_seq_len, H, dqk, dv, rab_time.numel(), code)
     if ws is None:
         n = hstu_attn_fwd_tree_workspace_bytes(p, cache, max_draft)
-        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
-    _on_device(q, k, v, seq_offsets, timestamps, parents, rab_pos, rab_time, out, ws,
-               *cache._arrays)
+        ws = q.new_empty(max(n, 256), dtype=torch.uint8)
+    _on_device(q, k, v, seq_offsets, timestamps, parents, rab_pos, rab_time, out, ws, cache.k)
     j = Jagged(offs, ts, None, rp, rt)
     _check(lib.hstu_attn_fwd_tree(ctypes.byref(p), ctypes.byref(j), ctypes.byref(cache._desc), par,
                                   int(max_draft), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(out),
