@@ -7,8 +7,6 @@
 // head.  d / 8 neighbouring lanes share a row, so that its largest magnitude
 // takes a few lane exchanges.  K rows go where they belong as they are; V goes
 // through LDS, because a page holds a feature's keys side by side.
-#include <type_traits>
-
 #include "kernels.h"
 
 namespace hstu {
@@ -137,22 +135,36 @@ struct Block {
 // offsets[b] / kBlk + 2 b: it touches at most (L + 2 kBlk - 2) / kBlk blocks, and
 // the next one's start is that far away whatever the offsets.
 __device__ __forceinline__ bool find_block(const CacheArgs& a, int64_t item, Block* o) {
-  const int lane = __lane_id();
-  int lo = 0, n = a.num_seqs;
-  while (n > 1) {
-    const int step = (n + 63) / 64;
-    const int at = lane * step;
-    const int64_t b = lo + (at < n ? at : 0);
-    const uint64_t below = __ballot(at < n && a.seq_offsets[b] / kBlk + 2 * b <= item);
-    const int last = below ? 63 - __builtin_clzll(below) : 0;
-    lo += last * step;
-    n = min(step, n - last * step);
+  const int lane = __lane_id(), B = a.num_seqs;
+  int lo = 0;
+  int64_t from, to, start = 0;
+  if (B < 64) {  // one load each: lane l knows sequence l
+    const int64_t off = lane <= B ? a.seq_offsets[lane] : 0;
+    const int64_t st = a.starts && lane < B ? a.starts[lane] : 0;
+    const uint64_t below = __ballot(lane < B && off / kBlk + 2 * lane <= item);
+    lo = below ? 63 - __builtin_clzll(below) : 0;
+    from = readlane64(off, lo);
+    to = readlane64(off, lo + 1);
+    start = readlane64(st, lo);
+  } else {
+    int n = B;
+    while (n > 1) {
+      const int step = (n + 63) / 64;
+      const int at = lane * step;
+      const int64_t b = lo + (at < n ? at : 0);
+      const uint64_t below = __ballot(at < n && a.seq_offsets[b] / kBlk + 2 * b <= item);
+      const int last = below ? 63 - __builtin_clzll(below) : 0;
+      lo += last * step;
+      n = min(step, n - last * step);
+    }
+    from = a.seq_offsets[lo];
+    to = a.seq_offsets[lo + 1];
+    if (a.starts) start = a.starts[lo];
   }
-  const int64_t from = a.seq_offsets[lo], to = a.seq_offsets[lo + 1];
   if (from < 0 || to > a.total_tokens) return false;
   // A start may be anything: beyond what pages can hold it only has to stay there.
   const int64_t far = (int64_t)1 << 42;
-  const int64_t start = a.starts ? max(-far, min(far, a.starts[lo])) : 0;
+  start = max(-far, min(far, start));
   const int64_t j = item - (from / kBlk + 2 * (int64_t)lo);
   o->seq = lo;
   o->first = ((start >> 6) + j) * kBlk;
@@ -170,219 +182,342 @@ __device__ __forceinline__ int64_t page_of(const CacheArgs& a, int b, int64_t x)
   return p >= 0 && p < a.num_pages ? p : -1;
 }
 
-template <typename E, int KIND, int D>
-__device__ __forceinline__ void write_side(const CacheArgs& a, const Block& blk, const int64_t* pages,
-                                           int head, bool values, char* tile) {
-  constexpr int LPR = D / 8;                       // lanes of a row
-  constexpr int CB = KIND == kCacheBf16 ? 2 : 1;   // bytes of a code
-  const int lane = threadIdx.x % LPR;
-  const int page_mask = (1 << a.lg_page) - 1;
-  const E* src = (const E*)(values ? a.v : a.k);
-  const int64_t stride = values ? a.v_stride : a.k_stride;
-  for (int r = threadIdx.x / LPR; r < kBlk; r += kThreads / LPR) {
-    const int64_t x = blk.first + r;
-    const bool on = x >= blk.lo && x < blk.hi;
-    Eight<E> e;
-    float f[8];
-    uint32_t top = 0;
-    if (on) {
-      e.load(src + (blk.row0 + x) * stride + (int64_t)head * D + 8 * lane);
-      e.get(f);
-    }
-    uint2 code{0u, 0u};
-    u32x4 wide{0u, 0u, 0u, 0u};
-    float scale = 1.0f;
-    if constexpr (KIND == kCacheBf16) {
-      if (on) wide = pack_bf16x8(f);
-    } else {
-      if (on)
+// A tile of V in LDS: kBlk rows of D codes, `ld` words apart, so that the four groups
+// of 16 keys that neighbouring lanes take lie in different quarters of the banks.
+template <int KIND, int D>
+struct Tile {
+  static constexpr int CB = KIND == kCacheBf16 ? 2 : 1;  // bytes of a code
+  static constexpr int FP = 4 / CB;                      // features of a word
+  static constexpr int ld = D * CB / 4 + 1;
+  uint32_t w[kBlk * ld];
+};
+
+// 16 words (keys m, FP features each) <-> FP rows (one feature, 16 keys each).
+__device__ __forceinline__ uint32_t bytes(uint32_t hi, uint32_t lo, uint32_t which) {
+  return __builtin_amdgcn_perm(hi, lo, which);
+}
+__device__ __forceinline__ void turn4(const uint32_t* a, uint32_t* o) {  // 4 x 4 bytes
+  const uint32_t x = bytes(a[1], a[0], 0x05010400u), y = bytes(a[1], a[0], 0x07030602u);
+  const uint32_t z = bytes(a[3], a[2], 0x05010400u), v = bytes(a[3], a[2], 0x07030602u);
+  o[0] = bytes(z, x, 0x05040100u);
+  o[1] = bytes(z, x, 0x07060302u);
+  o[2] = bytes(v, y, 0x05040100u);
+  o[3] = bytes(v, y, 0x07060302u);
+}
+__device__ __forceinline__ void turn2(const uint32_t* a, uint32_t* o) {  // 2 x 2 halfwords
+  o[0] = bytes(a[1], a[0], 0x05040100u);
+  o[1] = bytes(a[1], a[0], 0x07060302u);
+}
+
+// Where the codes of feature c and the keys of group g of a page's V lie.
+template <int CB, int D>
+__device__ __forceinline__ char* value_at(const CacheArgs& a, int64_t page, int head, int c,
+                                          int place) {
+  return (char*)a.vc + ((((page * a.num_heads + head) * D + c) << a.lg_page) + place) * CB;
+}
+
+// Largest magnitude of a row of D / 8 lanes with eight features each, as bits.
+template <int LPR>
+__device__ __forceinline__ uint32_t row_top(const float* f) {
+  uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
 #pragma unroll
-      for (int m = 1; m < LPR; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
-      if (on) code = quantise<KIND>(f, top, &scale);
-    }
-    const int64_t page = pages[r / kGroup];
-    const int64_t ph = page * a.num_heads + head;
-    const int place = (int)x & page_mask;
-    if (on && page >= 0) {
-      if constexpr (KIND != kCacheBf16)
-        if (lane == 0)
-          (values ? a.v_scale : a.k_scale)[(ph << a.lg_page) + place] = scale;
-      if (!values) {
-        char* dst = (char*)a.kc + (((ph << a.lg_page) + place) * D + 8 * lane) * CB;
-        if constexpr (KIND == kCacheBf16) *reinterpret_cast<u32x4*>(dst) = wide;
-        else *reinterpret_cast<uint2*>(dst) = code;
-      }
-    }
-    if (values) {
-      char* t = tile + (r * D + 8 * lane) * CB;
-      if constexpr (KIND == kCacheBf16) *reinterpret_cast<u32x4*>(t) = wide;
-      else *reinterpret_cast<uint2*>(t) = code;
-    }
-  }
-  if (!values) return;
-  __syncthreads();
-  using C = typename std::conditional<KIND == kCacheBf16, uint16_t, uint8_t>::type;
-  const C* t = (const C*)tile;
-  for (int i = threadIdx.x; i < D * (kBlk / kGroup); i += kThreads) {
-    const int c = i % D, g = i / D;
-    const int64_t page = pages[g];
-    const int64_t x0 = blk.first + g * kGroup;
-    if (page < 0 || x0 + kGroup <= blk.lo || x0 >= blk.hi) continue;
-    C* dst = (C*)a.vc + (((page * a.num_heads + head) * D + c) << a.lg_page) + ((int)x0 & page_mask);
-    union {
-      C c[kGroup];
-      u32x4 w[sizeof(C)];
-    } u;
+  for (int m = 1; m < LPR; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
+  return top;
+}
+
+// Eight codes of a row (in `w`, 2 or 4 words) and, from its first lane, its scale.
+template <typename E, int KIND, int LPR>
+__device__ __forceinline__ void encode(const Eight<E>& e, uint32_t* w, float* scale) {
+  float f[8];
+  e.get(f);
+  if constexpr (KIND == kCacheBf16) {
+    const u32x4 v = pack_bf16x8(f);
 #pragma unroll
-    for (int m = 0; m < kGroup; m++) u.c[m] = t[(g * kGroup + m) * D + c];
-    if (x0 >= blk.lo && x0 + kGroup <= blk.hi) {
-#pragma unroll
-      for (int m = 0; m < (int)sizeof(C); m++) reinterpret_cast<u32x4*>(dst)[m] = u.w[m];
-    } else {  // keys of other calls lie in the group
-#pragma unroll
-      for (int m = 0; m < kGroup; m++)
-        if (x0 + m >= blk.lo && x0 + m < blk.hi) dst[m] = u.c[m];
-    }
+    for (int i = 0; i < 4; i++) w[i] = v[i];
+  } else {
+    const uint2 v = quantise<KIND>(f, row_top<LPR>(f), scale);
+    w[0] = v.x;
+    w[1] = v.y;
   }
 }
 
-template <typename E, int KIND>
+template <typename E, int KIND, int DQK, int DV>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a) {
-  __shared__ __attribute__((aligned(16))) char tile[kBlk * 128 * (KIND == kCacheBf16 ? 2 : 1)];
+  using Tl = Tile<KIND, DV>;
+  constexpr int CB = Tl::CB, FP = Tl::FP;
+  constexpr int LK = DQK / 8, LV = DV / 8;                              // lanes of a row
+  constexpr int NK = kBlk * LK / kThreads, NV = kBlk * LV / kThreads;   // rows of a thread
+  __shared__ Tl tile;
   __shared__ int64_t pages[kBlk / kGroup];
-  const int head = blockIdx.y;
+  const int head = blockIdx.y, tid = threadIdx.x;
+  const int page_mask = (1 << a.lg_page) - 1;
   for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
     Block blk;
     if (!find_block(a, item, &blk)) continue;
+    // every load before any of their results is used
+    const int64_t page_of_group =
+        tid < kBlk / kGroup ? page_of(a, blk.seq, blk.first + tid * kGroup) : 0;
+    Eight<E> ek[NK], ev[NV];
+    auto there = [&](int r) { return blk.first + r >= blk.lo && blk.first + r < blk.hi; };
+#pragma unroll
+    for (int i = 0; i < NK; i++) {
+      const int r = tid / LK + i * (kThreads / LK);
+      ek[i] = Eight<E>{};
+      if (there(r))
+        ek[i].load((const E*)a.k + (blk.row0 + blk.first + r) * a.k_stride + (int64_t)head * DQK +
+                   8 * (tid % LK));
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int r = tid / LV + i * (kThreads / LV);
+      ev[i] = Eight<E>{};
+      if (there(r))
+        ev[i].load((const E*)a.v + (blk.row0 + blk.first + r) * a.v_stride + (int64_t)head * DV +
+                   8 * (tid % LV));
+    }
     __syncthreads();  // tile and pages of the item before
-    if (threadIdx.x < kBlk / kGroup)
-      pages[threadIdx.x] = page_of(a, blk.seq, blk.first + threadIdx.x * kGroup);
+    if (tid < kBlk / kGroup) pages[tid] = page_of_group;
     __syncthreads();
-    if (head == 0 && threadIdx.x < kBlk) {
-      const int64_t x = blk.first + threadIdx.x, page = pages[threadIdx.x / kGroup];
-      if (x >= blk.lo && x < blk.hi && page >= 0)
-        a.tc[(page << a.lg_page) + (x & ((1 << a.lg_page) - 1))] = a.ts[blk.row0 + x];
+    if (head == 0 && tid < kBlk && there(tid) && pages[tid / kGroup] >= 0) {
+      const int64_t x = blk.first + tid;
+      a.tc[(pages[tid / kGroup] << a.lg_page) + (x & page_mask)] = a.ts[blk.row0 + x];
     }
-    switch (a.d_qk) {
-      case 32: write_side<E, KIND, 32>(a, blk, pages, head, false, tile); break;
-      case 64: write_side<E, KIND, 64>(a, blk, pages, head, false, tile); break;
-      default: write_side<E, KIND, 128>(a, blk, pages, head, false, tile); break;
+#pragma unroll
+    for (int i = 0; i < NK; i++) {
+      const int r = tid / LK + i * (kThreads / LK);
+      uint32_t w[2 * CB];
+      float scale;
+      encode<E, KIND, LK>(ek[i], w, &scale);
+      const int64_t page = pages[r / kGroup];
+      if (!there(r) || page < 0) continue;
+      const int64_t row = ((page * a.num_heads + head) << a.lg_page) +
+                          ((blk.first + r) & page_mask);
+      char* dst = (char*)a.kc + (row * DQK + 8 * (tid % LK)) * CB;
+      if constexpr (CB == 2) {
+        *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
+      } else {
+        *reinterpret_cast<uint2*>(dst) = uint2{w[0], w[1]};
+        if (tid % LK == 0) a.k_scale[row] = scale;
+      }
     }
-    switch (a.d_v) {
-      case 32: write_side<E, KIND, 32>(a, blk, pages, head, true, tile); break;
-      case 64: write_side<E, KIND, 64>(a, blk, pages, head, true, tile); break;
-      default: write_side<E, KIND, 128>(a, blk, pages, head, true, tile); break;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int r = tid / LV + i * (kThreads / LV);
+      uint32_t w[2 * CB];
+      float scale;
+      encode<E, KIND, LV>(ev[i], w, &scale);
+#pragma unroll
+      for (int e = 0; e < 2 * CB; e++) tile.w[r * Tl::ld + 2 * CB * (tid % LV) + e] = w[e];
+      const int64_t page = pages[r / kGroup];
+      if (KIND != kCacheBf16 && tid % LV == 0 && there(r) && page >= 0)
+        a.v_scale[((page * a.num_heads + head) << a.lg_page) + ((blk.first + r) & page_mask)] =
+            scale;
+    }
+    __syncthreads();
+    // FP features and 16 keys at a time; neighbouring lanes take the groups of one page row
+    for (int u = tid; u < DV / FP * (kBlk / kGroup); u += kThreads) {
+      const int g = u % (kBlk / kGroup), c = u / (kBlk / kGroup) * FP;
+      const int64_t page = pages[g], x0 = blk.first + g * kGroup;
+      if (page < 0 || x0 + kGroup <= blk.lo || x0 >= blk.hi) continue;
+      uint32_t in[kGroup], out[FP][kGroup / FP];
+#pragma unroll
+      for (int m = 0; m < kGroup; m++) in[m] = tile.w[(g * kGroup + m) * Tl::ld + c / FP];
+#pragma unroll
+      for (int m = 0; m < kGroup / FP; m++) {
+        uint32_t o[FP];
+        if constexpr (FP == 4) turn4(in + FP * m, o);
+        else turn2(in + FP * m, o);
+#pragma unroll
+        for (int f = 0; f < FP; f++) out[f][m] = o[f];
+      }
+      const bool all = x0 >= blk.lo && x0 + kGroup <= blk.hi;
+#pragma unroll
+      for (int f = 0; f < FP; f++) {
+        char* dst = value_at<CB, DV>(a, page, head, c + f, (int)x0 & page_mask);
+        if (all) {
+#pragma unroll
+          for (int m = 0; m < CB; m++)
+            reinterpret_cast<u32x4*>(dst)[m] = u32x4{out[f][4 * m], out[f][4 * m + 1],
+                                                     out[f][4 * m + 2], out[f][4 * m + 3]};
+        } else {  // keys of other calls lie in the group
+#pragma unroll
+          for (int m = 0; m < kGroup; m++)
+            if (x0 + m >= blk.lo && x0 + m < blk.hi) {
+              const uint32_t v = out[f][m / FP] >> (8 * CB * (m % FP));
+              if constexpr (CB == 2) reinterpret_cast<uint16_t*>(dst)[m] = (uint16_t)v;
+              else reinterpret_cast<uint8_t*>(dst)[m] = (uint8_t)v;
+            }
+        }
+      }
     }
   }
 }
 
-template <typename E, int KIND, int D>
-__device__ __forceinline__ void read_side(const CacheArgs& a, const Block& blk, const int64_t* pages,
-                                          int head, bool values, char* tile) {
-  constexpr int LPR = D / 8;
-  constexpr int CB = KIND == kCacheBf16 ? 2 : 1;
-  const int page_mask = (1 << a.lg_page) - 1;
-  using C = typename std::conditional<KIND == kCacheBf16, uint16_t, uint8_t>::type;
-  if (values) {
-    C* t = (C*)tile;
-    for (int i = threadIdx.x; i < D * (kBlk / kGroup); i += kThreads) {
-      const int c = i % D, g = i / D;
-      const int64_t page = pages[g];
-      const int64_t x0 = blk.first + g * kGroup;
-      if (page < 0 || x0 + kGroup <= blk.lo || x0 >= blk.hi) continue;
-      const C* src = (const C*)a.vc + (((page * a.num_heads + head) * D + c) << a.lg_page) +
-                     ((int)x0 & page_mask);
-      union {
-        C c[kGroup];
-        u32x4 w[sizeof(C)];
-      } u;
-#pragma unroll
-      for (int m = 0; m < (int)sizeof(C); m++) u.w[m] = reinterpret_cast<const u32x4*>(src)[m];
-#pragma unroll
-      for (int m = 0; m < kGroup; m++) t[(g * kGroup + m) * D + c] = u.c[m];
+// Eight features of a row from its codes.
+template <typename E, int KIND>
+__device__ __forceinline__ void decode(const uint32_t* w, float scale, bool on, E* dst) {
+  float f[8] = {};
+  if (on) {
+    if constexpr (KIND == kCacheBf16) {
+      Eight<uint16_t> e;
+      e.raw = u32x4{w[0], w[1], w[2], w[3]};
+      e.get(f);
+    } else {
+      dequantise<KIND>(uint2{w[0], w[1]}, scale, f);
     }
-    __syncthreads();
   }
-  const int lane = threadIdx.x % LPR;
-  E* out = (E*)(values ? a.v_out : a.k_out);
-  const int64_t len = a.lengths[blk.seq];
-  for (int r = threadIdx.x / LPR; r < kBlk; r += kThreads / LPR) {
-    const int64_t x = blk.first + r;
-    if (x < blk.lo || x >= blk.hi) continue;
-    const int64_t page = pages[r / kGroup];
-    const int64_t ph = page * a.num_heads + head;
-    const int place = (int)x & page_mask;
-    float f[8] = {};
-    if (page >= 0 && x < len) {
-      const char* src = values ? tile + (r * D + 8 * lane) * CB
-                               : (const char*)a.kc + (((ph << a.lg_page) + place) * D + 8 * lane) * CB;
-      if constexpr (KIND == kCacheBf16) {
-        Eight<uint16_t> e;
-        e.load((const uint16_t*)src);
-        e.get(f);
+  if constexpr (sizeof(E) == 2) {
+    *reinterpret_cast<u32x4*>(dst) = pack_bf16x8(f);
+  } else {
+    *reinterpret_cast<f32x4*>(dst) = f32x4{f[0], f[1], f[2], f[3]};
+    *reinterpret_cast<f32x4*>(dst + 4) = f32x4{f[4], f[5], f[6], f[7]};
+  }
+}
+
+template <typename E, int KIND, int DQK, int DV>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a) {
+  using Tl = Tile<KIND, DV>;
+  constexpr int CB = Tl::CB, FP = Tl::FP;
+  constexpr int LK = DQK / 8, LV = DV / 8;
+  constexpr int NK = kBlk * LK / kThreads, NV = kBlk * LV / kThreads;
+  constexpr int kUnits = DV / FP * (kBlk / kGroup);
+  constexpr int NU = (kUnits + kThreads - 1) / kThreads;
+  __shared__ Tl tile;
+  __shared__ int64_t pages[kBlk / kGroup];
+  const int head = blockIdx.y, tid = threadIdx.x;
+  const int page_mask = (1 << a.lg_page) - 1;
+  for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+    Block blk;
+    if (!find_block(a, item, &blk)) continue;
+    const int64_t len = a.lengths[blk.seq];
+    __syncthreads();  // tile and pages of the item before
+    if (tid < kBlk / kGroup) pages[tid] = page_of(a, blk.seq, blk.first + tid * kGroup);
+    __syncthreads();
+    auto wanted = [&](int r) { return blk.first + r >= blk.lo && blk.first + r < blk.hi; };
+    auto there = [&](int r) {
+      return wanted(r) && blk.first + r < len && pages[r / kGroup] >= 0;
+    };
+    auto row_of = [&](int r) {
+      return ((pages[r / kGroup] * a.num_heads + head) << a.lg_page) +
+             ((blk.first + r) & page_mask);
+    };
+    // every load before any of their results is used
+    uint32_t wk[NK][2 * CB];
+    float sk[NK], sv[NV];
+#pragma unroll
+    for (int i = 0; i < NK; i++) {
+      const int r = tid / LK + i * (kThreads / LK);
+      sk[i] = 1.0f;
+#pragma unroll
+      for (int e = 0; e < 2 * CB; e++) wk[i][e] = 0;
+      if (!there(r)) continue;
+      const int64_t row = row_of(r);
+      const char* src = (const char*)a.kc + (row * DQK + 8 * (tid % LK)) * CB;
+      if constexpr (CB == 2) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(src);
+#pragma unroll
+        for (int e = 0; e < 4; e++) wk[i][e] = v[e];
       } else {
-        const float s = (values ? a.v_scale : a.k_scale)[(ph << a.lg_page) + place];
-        dequantise<KIND>(*reinterpret_cast<const uint2*>(src), s, f);
+        const uint2 v = *reinterpret_cast<const uint2*>(src);
+        wk[i][0] = v.x;
+        wk[i][1] = v.y;
+        sk[i] = a.k_scale[row];
       }
     }
-    E* dst = out + ((blk.row0 + x) * a.num_heads + head) * D + 8 * lane;
-    if constexpr (sizeof(E) == 2) {
-      *reinterpret_cast<u32x4*>(dst) = pack_bf16x8(f);
-    } else {
-      *reinterpret_cast<f32x4*>(dst) = f32x4{f[0], f[1], f[2], f[3]};
-      *reinterpret_cast<f32x4*>(dst + 4) = f32x4{f[4], f[5], f[6], f[7]};
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int r = tid / LV + i * (kThreads / LV);
+      sv[i] = KIND != kCacheBf16 && there(r) ? a.v_scale[row_of(r)] : 1.0f;
+    }
+    u32x4 wv[NU][FP][CB];
+#pragma unroll
+    for (int n = 0; n < NU; n++) {
+      const int u = tid + n * kThreads;
+      const int g = u % (kBlk / kGroup), c = u / (kBlk / kGroup) * FP;
+      const int64_t page = pages[g], x0 = blk.first + g * kGroup;
+      const bool on = u < kUnits && page >= 0 && x0 + kGroup > blk.lo && x0 < blk.hi;
+#pragma unroll
+      for (int f = 0; f < FP; f++)
+#pragma unroll
+        for (int m = 0; m < CB; m++) {
+          wv[n][f][m] = zero_u32x4();
+          if (on)
+            wv[n][f][m] = reinterpret_cast<const u32x4*>(
+                value_at<CB, DV>(a, page, head, c + f, (int)x0 & page_mask))[m];
+        }
+    }
+    if (head == 0 && a.ts_out && tid < kBlk && wanted(tid)) {
+      const int64_t x = blk.first + tid;
+      a.ts_out[blk.row0 + x] =
+          there(tid) ? a.tc[(pages[tid / kGroup] << a.lg_page) + (x & page_mask)] : 0;
+    }
+#pragma unroll
+    for (int n = 0; n < NU; n++) {
+      const int u = tid + n * kThreads;
+      const int g = u % (kBlk / kGroup), c = u / (kBlk / kGroup) * FP;
+      if (u >= kUnits) break;
+#pragma unroll
+      for (int m = 0; m < kGroup / FP; m++) {
+        uint32_t in[FP], out[FP];
+#pragma unroll
+        for (int f = 0; f < FP; f++) in[f] = wv[n][f][m / 4][m % 4];
+        if constexpr (FP == 4) turn4(in, out);
+        else turn2(in, out);
+#pragma unroll
+        for (int f = 0; f < FP; f++)
+          tile.w[(g * kGroup + FP * m + f) * Tl::ld + c / FP] = out[f];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NK; i++) {
+      const int r = tid / LK + i * (kThreads / LK);
+      if (!wanted(r)) continue;
+      decode<E, KIND>(wk[i], sk[i], there(r),
+                      (E*)a.k_out + ((blk.row0 + blk.first + r) * a.num_heads + head) * DQK +
+                          8 * (tid % LK));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int r = tid / LV + i * (kThreads / LV);
+      if (!wanted(r)) continue;
+      uint32_t w[2 * CB];
+#pragma unroll
+      for (int e = 0; e < 2 * CB; e++) w[e] = tile.w[r * Tl::ld + 2 * CB * (tid % LV) + e];
+      decode<E, KIND>(w, sv[i], there(r),
+                      (E*)a.v_out + ((blk.row0 + blk.first + r) * a.num_heads + head) * DV +
+                          8 * (tid % LV));
     }
   }
 }
 
 template <typename E, int KIND>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a) {
-  __shared__ __attribute__((aligned(16))) char tile[kBlk * 128 * (KIND == kCacheBf16 ? 2 : 1)];
-  __shared__ int64_t pages[kBlk / kGroup];
-  const int head = blockIdx.y;
-  for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
-    Block blk;
-    if (!find_block(a, item, &blk)) continue;
-    __syncthreads();
-    if (threadIdx.x < kBlk / kGroup)
-      pages[threadIdx.x] = page_of(a, blk.seq, blk.first + threadIdx.x * kGroup);
-    __syncthreads();
-    if (head == 0 && a.ts_out && threadIdx.x < kBlk) {
-      const int64_t x = blk.first + threadIdx.x, page = pages[threadIdx.x / kGroup];
-      if (x >= blk.lo && x < blk.hi)
-        a.ts_out[blk.row0 + x] = page >= 0 && x < a.lengths[blk.seq]
-                                     ? a.tc[(page << a.lg_page) + (x & ((1 << a.lg_page) - 1))]
-                                     : 0;
-    }
-    switch (a.d_qk) {
-      case 32: read_side<E, KIND, 32>(a, blk, pages, head, false, tile); break;
-      case 64: read_side<E, KIND, 64>(a, blk, pages, head, false, tile); break;
-      default: read_side<E, KIND, 128>(a, blk, pages, head, false, tile); break;
-    }
-    switch (a.d_v) {
-      case 32: read_side<E, KIND, 32>(a, blk, pages, head, true, tile); break;
-      case 64: read_side<E, KIND, 64>(a, blk, pages, head, true, tile); break;
-      default: read_side<E, KIND, 128>(a, blk, pages, head, true, tile); break;
-    }
-  }
-}
-
-template <typename E>
-hipError_t run(const CacheArgs& a, int kind, bool write, dim3 grid, hipStream_t s) {
+hipError_t run(const CacheArgs& a, bool write, dim3 grid, hipStream_t s) {
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a);
     return hipGetLastError();
   };
-  if (write) {
-    if (kind == kCacheBf16) return go(cache_write_kernel<E, kCacheBf16>);
-    if (kind == kCacheInt8) return go(cache_write_kernel<E, kCacheInt8>);
-    return go(cache_write_kernel<E, kCacheE4m3>);
-  }
-  if (kind == kCacheBf16) return go(cache_read_kernel<E, kCacheBf16>);
-  if (kind == kCacheInt8) return go(cache_read_kernel<E, kCacheInt8>);
-  return go(cache_read_kernel<E, kCacheE4m3>);
+#define HSTU_CACHE_V(DQK, DV)                                    \
+  return write ? go(cache_write_kernel<E, KIND, DQK, DV>)        \
+               : go(cache_read_kernel<E, KIND, DQK, DV>);
+#define HSTU_CACHE(DQK)                           \
+  if (a.d_v == 32) { HSTU_CACHE_V(DQK, 32) }      \
+  if (a.d_v == 64) { HSTU_CACHE_V(DQK, 64) }      \
+  HSTU_CACHE_V(DQK, 128)
+  if (a.d_qk == 32) { HSTU_CACHE(32) }
+  if (a.d_qk == 64) { HSTU_CACHE(64) }
+  HSTU_CACHE(128)
+#undef HSTU_CACHE
+#undef HSTU_CACHE_V
+}
+
+template <typename E>
+hipError_t run(const CacheArgs& a, int kind, bool write, dim3 grid, hipStream_t s) {
+  return kind == kCacheBf16   ? run<E, kCacheBf16>(a, write, grid, s)
+         : kind == kCacheInt8 ? run<E, kCacheInt8>(a, write, grid, s)
+                              : run<E, kCacheE4m3>(a, write, grid, s);
 }
 
 }  // namespace
