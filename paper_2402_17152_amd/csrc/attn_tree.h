@@ -44,24 +44,24 @@ namespace tree {
 
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;       // keys whose scales, times and pages are held
-constexpr int kWindow = 512;      // entries of rab_pos that are held
+constexpr int kWindow = 512;      // entries of rab_pos that are held at most
 constexpr float kNegLog2e = -kLog2e;
 
 // What is known of 64 keys: each row's time bucket is the same for all; the time
 // differences fit 32 bits; all of the first, the second 32 keys are there.
 enum { kOneBucket = 1, kNear = 2, kWhole = 4 };
 
-// What the waves of a workgroup know of kBlock keys; HG: heads, ROWS: drafted rows.
-template <int HG, int ROWS>
+// What the waves of a workgroup know of kBlock keys; HG: heads, ROWS: drafted rows,
+// WIN: entries of rab_pos (kBlock and as many as the depths of the rows can differ).
+template <int HG, int ROWS, int WIN>
 struct Keys {
-  static constexpr int heads = HG;
+  static constexpr int spread = WIN - kBlock;
   float scales[2][HG][kBlock];     // k (times -log2(e)) and v
-  float window[4][kWindow + 8];    // part of rab_pos (times -log2(e)), four shifted copies
-  int64_t time[kBlock];
-  int time32[kBlock];              // its low word
+  float window[4][WIN + 4];        // part of rab_pos (times -log2(e)), four shifted copies
+  int time[2][kBlock];             // low and high words
   int64_t rows16[kBlock / 16];     // first cache row of 16 keys for head 0
   int left16[kBlock / 16];         // how many of them are there; of none, row 0 is read
-  float uniform[4][ROWS];          // the rows' entry of rtime for 64 keys (kOneBucket)
+  uint8_t bucket[4][ROWS];         // the rows' time bucket for 64 keys (kOneBucket)
   int about[4];                    // what is known of 64 keys
 };
 
@@ -282,12 +282,12 @@ __device__ __forceinline__ void put_rows(const TreeArgs& a, const Part& w, int k
 }
 
 // The rest of what is known of them.
-template <bool Q8, int HG, int ROWS>
+template <bool Q8, int HG, int ROWS, int WIN>
 __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const Rows<ROWS>& rows,
-                                         const Ahead<HG>& h, Keys<HG, ROWS>* k) {
+                                         const Ahead<HG>& h, Keys<HG, ROWS, WIN>* k) {
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  k->time[tid] = h.time;
-  k->time32[tid] = (int)h.time;
+  k->time[0][tid] = (int)h.time;
+  k->time[1][tid] = (int)(h.time >> 32);
   if constexpr (Q8)
 #pragma unroll
     for (int x = 0; x < HG; x++)
@@ -303,7 +303,7 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
 #pragma unroll
       for (int c = 0; c < 4; c++) {
         const int x = tid + e * kThreads - c;
-        if (x >= 0) k->window[c][x] = h.pos[e] * kNegLog2e;
+        if (x >= 0 && x < WIN) k->window[c][x] = h.pos[e] * kNegLog2e;
       }
   // What the rows' times have in common with those of this wave's 64 keys:
   // |dt| is monotone in the key's time on either side of 0.
@@ -318,7 +318,7 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
     const int by = time_bucket64(y, a.ja.num_buckets);
     one &= bx == by && ((x >= 0) == (y >= 0) || bx == 0);
     near &= x == (int)x && y == (int)y && (int)x != INT32_MIN && (int)y != INT32_MIN;
-    k->uniform[wave][i] = rows.rtime[by];
+    k->bucket[wave][i] = (uint8_t)by;
   }
   const int all_one = __ballot(!one) == 0 ? kOneBucket : 0;
   const int all_near = __ballot(!near) == 0 ? kNear : 0;
@@ -337,7 +337,8 @@ __device__ __forceinline__ bool bound_depths(const TreeArgs& a, Part* w) {
 
 // Depths of this lane's rows w0 + 16 m + r (0 where there is none), and, where
 // bound_depths() does not know them, the window's.  parent: of node `lane`.
-template <int R>
+// SMALL: max_draft is at most 64.
+template <bool SMALL, int R>
 __device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, int64_t parent,
                                             short2* node, int* depth) {
   const int lane = threadIdx.x % 64, r = lane % 16;
@@ -345,31 +346,33 @@ __device__ __forceinline__ void find_depths(const TreeArgs& a, Part* w, int w0, 
 #pragma unroll
   for (int m = 0; m < R; m++) depth[m] = 0;
   if (!a.parents) return;
-  if (nodes <= 64) {
+  if (SMALL || nodes <= 64) {
     const int d = walk64(parent >= 0 && parent < lane ? (int)parent : -1);
 #pragma unroll
     for (int m = 0; m < R; m++) {
       const int x = __shfl(d, (w->r0 + w0 + 16 * m + r) & 63, 64);
       if (w0 + 16 * m + r < w->rows) depth[m] = x;
     }
-    if (!w->windowed) {  // depths below 64
+    if (!SMALL && !w->windowed) {  // depths below 64
       w->windowed = true;
       w->deep = 63;
     }
     return;
   }
-  walk(a.parents + w->o, nodes, node);
+  if constexpr (!SMALL) {
+    walk(a.parents + w->o, nodes, node);
 #pragma unroll
-  for (int m = 0; m < R; m++)
-    if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
-  if (!w->windowed) {
-    int deep = 0, flat = kMaxDraft;
-    for (int i = w->r0 + lane; i < nodes; i += 64) {
-      deep = max(deep, (int)node[i].y);
-      flat = min(flat, (int)node[i].y);
+    for (int m = 0; m < R; m++)
+      if (w0 + 16 * m + r < w->rows) depth[m] = node[w->r0 + w0 + 16 * m + r].y;
+    if (!w->windowed) {
+      int deep = 0, flat = kMaxDraft;
+      for (int i = w->r0 + lane; i < nodes; i += 64) {
+        deep = max(deep, (int)node[i].y);
+        flat = min(flat, (int)node[i].y);
+      }
+      w->deep = wave_extreme<true>(deep);
+      w->windowed = w->deep - wave_extreme<false>(flat) < kWindow - kBlock;
     }
-    w->deep = wave_extreme<true>(deep);
-    w->windowed = w->deep - wave_extreme<false>(flat) < kWindow - kBlock;
   }
 }
 
@@ -393,16 +396,16 @@ __device__ __forceinline__ void load_q(const TreeArgs& a, const Part& w, int w0,
 }
 
 // -log2(e) times the bias of this lane's rows and the eight keys k0 + at ..
-template <int R, int HG, int ROWS>
+template <int R, int HG, int ROWS, int WIN>
 __device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, const Rows<ROWS>& rows,
-                                          const Keys<HG, ROWS>& k, int about, int k0, int at, int w0,
+                                          const Keys<HG, ROWS, WIN>& k, int about, int k0, int at, int w0,
                                           const int* depth, f32x4 (&bv)[R][2]) {
   const int r = threadIdx.x % 16;
   if (w.windowed && (about & kOneBucket)) {
 #pragma unroll
     for (int m = 0; m < R; m++) {
-      const float one = k.uniform[at / 64][w0 + 16 * m + r];
-      const int shift = max(0, min(w.deep - depth[m], kWindow - kBlock - 1));
+      const float one = rows.rtime[k.bucket[at / 64][w0 + 16 * m + r]];
+      const int shift = max(0, min(w.deep - depth[m], WIN - kBlock - 1));
       const float* win = &k.window[shift & 3][(shift & ~3) + at];
 #pragma unroll
       for (int x = 0; x < 2; x++) bv[m][x] = *reinterpret_cast<const f32x4*>(win + 4 * x) + one;
@@ -413,17 +416,20 @@ __device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, cons
 #pragma unroll
   for (int m = 0; m < R; m++) {
     const int64_t rt = rows.time[w0 + 16 * m + r];
-    const int shift = max(0, min(w.deep - depth[m], kWindow - kBlock - 1));
+    const int shift = max(0, min(w.deep - depth[m], WIN - kBlock - 1));
     int bucket[8];
     if (about & kNear) {
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        const int dt = (int)rt - k.time32[at + i];
+        const int dt = (int)rt - k.time[0][at + i];
         bucket[i] = min(31 - __clz(max(1, max(dt, -dt))), a.ja.num_buckets - 1);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; i++) bucket[i] = time_bucket64(rt - k.time[at + i], a.ja.num_buckets);
+      for (int i = 0; i < 8; i++) {
+        const int64_t kt = (int64_t)k.time[1][at + i] << 32 | (uint32_t)k.time[0][at + i];
+        bucket[i] = time_bucket64(rt - kt, a.ja.num_buckets);
+      }
     }
     float pos[8];
     if (w.windowed) {
@@ -568,16 +574,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   // Tiles a wave has under way: the compute units' share of the memory's latency is
   // 43 KB; two tiles where the registers hold them.
   constexpr int P = H4 && R == 1 && DQK + DV <= 128 ? 2 : 1;
-  using Kb = Keys<4, 16 * R>;
+  using Kb = Keys<4, 16 * R, kBlock + 32>;
   __shared__ __attribute__((aligned(16))) union {
     Kb kb[2];
     float sums[2 * 16 * R * DV];
-    struct {
-      Kb first;
-      short2 node[kMaxDraft];
-    };
   } sh;
-  static_assert(sizeof(Kb) >= sizeof(sh.node), "the depths fit where the second block goes");
   __shared__ Rows<16 * R> rs;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Part w;
@@ -628,7 +629,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   // come back in order, and the few small ones should not wait for the many.
   Ahead<4> h;
   fetch<Q8>(a, w, w.from, first_page, &h);
-  if (bound_depths(a, &w)) fetch_pos(a, w, w.from, &h);
+  bound_depths(a, &w);  // there are at most 32 drafted tokens
+  fetch_pos(a, w, w.from, &h);
   bf16x8 q[R][KS];
   load_q<KIND, DQK, R>(a, w, 0, head, q);
   const float bucket_bias = tid < a.ja.num_buckets ? a.ja.rab_time[tid] : 0.0f;
@@ -648,10 +650,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
     for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   rs.rtime[tid] = bucket_bias * kNegLog2e;
   if (tid < 16 * R) rs.time[tid] = row_time;
-  const bool known = w.windowed;
   int depth[R];
-  find_depths<R>(a, &w, 0, parent, sh.node, depth);
-  if (!known) fetch_pos(a, w, w.from, &h);
+  find_depths<true, R>(a, &w, 0, parent, nullptr, depth);
   __syncthreads();  // rs
   put_keys<Q8>(a, w, rs, h, &sh.kb[0]);
   if (w.from + kBlock < w.to) {
@@ -800,7 +800,7 @@ struct Tile {
 };
 
 template <int KIND, int DQK, int DV, int R>
-__global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeArgs a,
+__global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kernel(const TreeArgs a,
                                                                      const TreeSplit sp) {
   using Tl = Tile<KIND, DQK, DV>;
   constexpr bool Q8 = KIND != kCacheBf16;
@@ -809,10 +809,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   constexpr int KL = (Tl::kPieces + kThreads - 1) / kThreads;  // pieces a thread loads
   constexpr int VL = (Tl::vPieces + kThreads - 1) / kThreads;
   constexpr int TB = kBlock / T;                               // tiles of a block
-  // Tiles under way: two where the rows are few and the cache's bytes are the bound
-  // (a tile of 16 KB under way in each of two workgroups holds a CU to 4 TB/s).
-  constexpr int P = R == 1 ? 2 : 1;
-  using Kb = Keys<1, 64 * R>;
+  using Kb = Keys<1, 64 * R, R == 1 ? kBlock + 64 : kWindow>;
   __shared__ __attribute__((aligned(16))) Kb kb[2];
   __shared__ __attribute__((aligned(16))) Tl tiles[2];
   __shared__ Rows<64 * R> rs;
@@ -840,17 +837,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   const int64_t parent = a.parents && lane < w.r0 + w.rows ? a.parents[w.o + lane] : -1;
   rs.rtime[tid] = bucket_bias * kNegLog2e;
   if (tid < 64 * R) rs.time[tid] = row_time;
-  // Tile j of the chunk: loads into one of P sets of registers, then into LDS.
+  // Tile j of the chunk: loads into registers, then into LDS.
   const int count = (w.to - w.from + T - 1) / T;
-  u32x4 kr[P][KL], vr[P][VL];
-  auto load = [&](int j, int set) {
+  u32x4 kr[KL], vr[VL];
+  auto load = [&](int j) {
     const Kb& k = kb[j / TB % 2];
     const int t0 = j % TB * T;
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads, at = t0 + x / KP;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      kr[set][e] = *reinterpret_cast<const u32x4*>(
+      kr[e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.kc +
           (k.rows16[at / 16] + ((int64_t)head << lg) + at % 16) * (DQK * CB) + x % KP * 16);
     }
@@ -860,7 +857,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
       const int64_t row = k.rows16[at / 16];
       const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
-      vr[set][e] = *reinterpret_cast<const u32x4*>(
+      vr[e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.vc + (((((row >> lg) + head) * DV + x / 4) << lg) + place) * CB);
     }
   };
@@ -869,55 +866,52 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
     const int about = __builtin_amdgcn_readfirstlane(kb[j / TB % 2].about[t0 / 64]);
     return (about & all) == all;
   };
-  auto store = [&](int j, int set) {
+  auto store = [&](int j) {
     Tl& tl = tiles[j % 2];
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[set][e];
+      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[e];
     }
     if (!is_whole(j)) {  // codes behind the last key count as zeros
       const Kb& k = kb[j / TB % 2];
       const int at = j % TB * T + GK * (tid % 4);
       const int left = max(0, min(GK, k.left16[at / 16] - at % 16));
 #pragma unroll
-      for (int e = 0; e < VL; e++) vr[set][e] = cut<CB>(vr[set][e], left);
+      for (int e = 0; e < VL; e++) vr[e] = cut<CB>(vr[e], left);
     }
 #pragma unroll
     for (int e = 0; e < VL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
-      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4 / NC, x / 4 % NC, x % 4)) = vr[set][e];
+      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4 / NC, x / 4 % NC, x % 4)) = vr[e];
     }
   };
 
   int depth[R];
   static_assert(sizeof(tiles) >= kMaxDraft * sizeof(short2), "the depths fit where the tiles go");
   const bool known = w.windowed;
-  find_depths<R>(a, &w, w0, parent, reinterpret_cast<short2*>(tiles), depth);
+  find_depths<R == 1, R>(a, &w, w0, parent, reinterpret_cast<short2*>(tiles), depth);
   if (!known) fetch_pos(a, w, w.from, &h);
   put_rows(a, w, w.from, h.page, &kb[0]);
   __syncthreads();
   if (count > 0) {
-    load(0, 0);
+    load(0);
     put_keys<Q8>(a, w, rs, h, &kb[0]);
     if (w.from + kBlock < w.to) {
       fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
       fetch_pos(a, w, w.from + kBlock, &h);
     }
     __syncthreads();
-    store(0, 0);
-    if (P == 2 && count > 1) load(1, 1);
+    store(0);
     __syncthreads();
   }
-  auto turn = [&](int j, auto odd) {
-    // P tiles ahead, in the registers of the tile that is in LDS by now
-    constexpr int set = P == 2 ? decltype(odd)::value : 0;
-    if (j + P < count) load(j + P, set);
+  for (int j = 0; j < count; j++) {
+    if (j + 1 < count) load(j + 1);
     // the next block's keys, before their first tile's loads
     const int k1 = w.from + (j / TB + 1) * kBlock;
-    if (j % TB == TB - P - 2 && k1 < w.to) {
+    if (j % TB == TB - 3 && k1 < w.to) {
       put_rows(a, w, k1, h.page, &kb[(j / TB + 1) % 2]);
       put_keys<Q8>(a, w, rs, h, &kb[(j / TB + 1) % 2]);
       if (k1 + kBlock < w.to) {
@@ -996,12 +990,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
         }
       }
     }
-    if (j + 1 < count) store(j + 1, P == 2 ? 1 - set : 0);
+    if (j + 1 < count) store(j + 1);
     __syncthreads();
-  };
-  for (int j = 0; j < count; j += 2) {
-    turn(j, std::integral_constant<int, 0>{});
-    if (j + 1 < count) turn(j + 1, std::integral_constant<int, 1>{});
   }
   if (idle) return;
   if (sp.last) put_out<KIND, DQK, DV, R>(a, w, w0, head, q, acc);
