@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
                                                                int waves) {
   constexpr int LK = DQK / 8, LV = DV / 8;  // lanes of a K row, of a V row
   extern __shared__ short space[];
-  __shared__ float weight[kThreads / 64][64];
+  __shared__ float score[kThreads / 64][64];
   __shared__ float rest[kThreads / 64 - 1][DV];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int H = a.ja.num_heads;
@@ -174,31 +174,37 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
       float q[8] = {};
       add8(q, q8, 1.0f);
       const int64_t time = forest.time(a, o, i);
+      // 64 nodes of the way at a time: lane y knows node y, its bias and its weight,
+      // so that the loops over keys and values wait for nothing but their loads.
       for (int w0 = 0; w0 < count; w0 += 64) {
-        const int here = min(64, count - w0);
+        const int here = min(64, count - w0), mine = min(lane, here - 1);
+        const int node = above(w0 + mine);
+        const float bias =
+            a.ja.rab_pos[max(0, N - 1 - (w0 + mine))] +
+            a.ja.rab_time[time_bucket64(time - forest.time(a, o, node), a.ja.num_buckets)];
+#pragma unroll 4
         for (int y0 = 0; y0 < here; y0 += 64 / LK) {
-          const int y = min(y0 + lane / LK, here - 1);
-          const int n = above(w0 + y);
-          const int64_t dt = time - forest.time(a, o, n);
           float k[8] = {};
-          add8(k, key(n), 1.0f);
+          add8(k, key(__shfl(node, min(y0 + lane / LK, here - 1), 64)), 1.0f);
           float s = 0.0f;
 #pragma unroll
           for (int e = 0; e < 8; e++) s = fmaf(q[e], k[e], s);
 #pragma unroll
           for (int m = 1; m < LK; m *= 2) s += __shfl_xor(s, m, 64);
-          s += a.ja.rab_pos[max(0, N - 1 - (w0 + y))] +
-               a.ja.rab_time[time_bucket64(dt, a.ja.num_buckets)];
-          if (lane % LK == 0 && y0 + lane / LK < here) weight[wave][y] = s * sigmoid_fast(s);
+          if (lane % LK == 0) score[wave][y0 + lane / LK] = s;
         }
         __builtin_amdgcn_wave_barrier();
+        float p = score[wave][mine] + bias;
+        p *= sigmoid_fast(p);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
         for (int y0 = 0; y0 < here; y0 += 64 / LV) {
-          const int y = y0 + lane / LV;
-          const bool on = y < here;
-          const u32x4 v = w0 + y0 == 0 ? v8 : value(above(w0 + min(y, here - 1)));
-          if (on) add8(x, v, weight[wave][y]);
+          const int y = min(y0 + lane / LV, here - 1);
+          const int n = __shfl(node, y, 64);
+          const float w = __shfl(p, y, 64);
+          const u32x4 v = w0 + y0 == 0 ? v8 : value(n);
+          if (y0 + lane / LV < here) add8(x, v, w);
         }
-        __builtin_amdgcn_wave_barrier();
       }
     }
 #pragma unroll
