@@ -61,7 +61,7 @@ struct Keys {
   int time[2][kBlock];             // low and high words
   int64_t rows16[kBlock / 16];     // first cache row of 16 keys for head 0
   int left16[kBlock / 16];         // how many of them are there; of none, row 0 is read
-  uint8_t bucket[4][ROWS];         // the rows' time bucket for 64 keys (kOneBucket)
+  float uniform[4][ROWS];          // the rows' entry of rtime for 64 keys (kOneBucket)
   int about[4];                    // what is known of 64 keys
 };
 
@@ -318,7 +318,7 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
     const int by = time_bucket64(y, a.ja.num_buckets);
     one &= bx == by && ((x >= 0) == (y >= 0) || bx == 0);
     near &= x == (int)x && y == (int)y && (int)x != INT32_MIN && (int)y != INT32_MIN;
-    k->bucket[wave][i] = (uint8_t)by;
+    k->uniform[wave][i] = rows.rtime[by];
   }
   const int all_one = __ballot(!one) == 0 ? kOneBucket : 0;
   const int all_near = __ballot(!near) == 0 ? kNear : 0;
@@ -404,7 +404,7 @@ __device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, cons
   if (w.windowed && (about & kOneBucket)) {
 #pragma unroll
     for (int m = 0; m < R; m++) {
-      const float one = rows.rtime[k.bucket[at / 64][w0 + 16 * m + r]];
+      const float one = k.uniform[at / 64][w0 + 16 * m + r];
       const int shift = max(0, min(w.deep - depth[m], WIN - kBlock - 1));
       const float* win = &k.window[shift & 3][(shift & ~3) + at];
 #pragma unroll
@@ -800,7 +800,7 @@ struct Tile {
 };
 
 template <int KIND, int DQK, int DV, int R>
-__global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kernel(const TreeArgs a,
+__global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeArgs a,
                                                                      const TreeSplit sp) {
   using Tl = Tile<KIND, DQK, DV>;
   constexpr bool Q8 = KIND != kCacheBf16;
@@ -809,6 +809,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
   constexpr int KL = (Tl::kPieces + kThreads - 1) / kThreads;  // pieces a thread loads
   constexpr int VL = (Tl::vPieces + kThreads - 1) / kThreads;
   constexpr int TB = kBlock / T;                               // tiles of a block
+  constexpr int P = R == 1 ? 2 : 1;                            // tiles under way
   using Kb = Keys<1, 64 * R, R == 1 ? kBlock + 64 : kWindow>;
   __shared__ __attribute__((aligned(16))) Kb kb[2];
   __shared__ __attribute__((aligned(16))) Tl tiles[2];
@@ -837,17 +838,17 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
   const int64_t parent = a.parents && lane < w.r0 + w.rows ? a.parents[w.o + lane] : -1;
   rs.rtime[tid] = bucket_bias * kNegLog2e;
   if (tid < 64 * R) rs.time[tid] = row_time;
-  // Tile j of the chunk: loads into registers, then into LDS.
+  // Tile j of the chunk: loads into one of P sets of registers, then into LDS.
   const int count = (w.to - w.from + T - 1) / T;
-  u32x4 kr[KL], vr[VL];
-  auto load = [&](int j) {
+  u32x4 kr[P][KL], vr[P][VL];
+  auto load = [&](int j, int set) {
     const Kb& k = kb[j / TB % 2];
     const int t0 = j % TB * T;
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads, at = t0 + x / KP;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      kr[e] = *reinterpret_cast<const u32x4*>(
+      kr[set][e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.kc +
           (k.rows16[at / 16] + ((int64_t)head << lg) + at % 16) * (DQK * CB) + x % KP * 16);
     }
@@ -857,7 +858,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
       const int64_t row = k.rows16[at / 16];
       const int place = (int)(row & ((1 << lg) - 1)) + at % 16;
-      vr[e] = *reinterpret_cast<const u32x4*>(
+      vr[set][e] = *reinterpret_cast<const u32x4*>(
           (const char*)a.c.vc + (((((row >> lg) + head) * DV + x / 4) << lg) + place) * CB);
     }
   };
@@ -866,26 +867,26 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
     const int about = __builtin_amdgcn_readfirstlane(kb[j / TB % 2].about[t0 / 64]);
     return (about & all) == all;
   };
-  auto store = [&](int j) {
+  auto store = [&](int j, int set) {
     Tl& tl = tiles[j % 2];
 #pragma unroll
     for (int e = 0; e < KL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::kPieces % kThreads && x >= Tl::kPieces) break;
-      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[e];
+      *reinterpret_cast<u32x4*>(tl.k + Tl::k_at(x / KP, x % KP)) = kr[set][e];
     }
     if (!is_whole(j)) {  // codes behind the last key count as zeros
       const Kb& k = kb[j / TB % 2];
       const int at = j % TB * T + GK * (tid % 4);
       const int left = max(0, min(GK, k.left16[at / 16] - at % 16));
 #pragma unroll
-      for (int e = 0; e < VL; e++) vr[e] = cut<CB>(vr[e], left);
+      for (int e = 0; e < VL; e++) vr[set][e] = cut<CB>(vr[set][e], left);
     }
 #pragma unroll
     for (int e = 0; e < VL; e++) {
       const int x = tid + e * kThreads;
       if (Tl::vPieces % kThreads && x >= Tl::vPieces) break;
-      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4 / NC, x / 4 % NC, x % 4)) = vr[e];
+      *reinterpret_cast<u32x4*>(tl.v + Tl::v_at(x / 4 / NC, x / 4 % NC, x % 4)) = vr[set][e];
     }
   };
 
@@ -897,21 +898,24 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
   put_rows(a, w, w.from, h.page, &kb[0]);
   __syncthreads();
   if (count > 0) {
-    load(0);
+    load(0, 0);
     put_keys<Q8>(a, w, rs, h, &kb[0]);
     if (w.from + kBlock < w.to) {
       fetch<Q8>(a, w, w.from + kBlock, fetch_page(a, w, w.from + kBlock), &h);
       fetch_pos(a, w, w.from + kBlock, &h);
     }
     __syncthreads();
-    store(0);
+    store(0, 0);
+    if (P == 2 && count > 1) load(1, 1);
     __syncthreads();
   }
-  for (int j = 0; j < count; j++) {
-    if (j + 1 < count) load(j + 1);
+  auto turn = [&](int j, auto odd) {
+    // P tiles ahead, into the registers of the tile that is in LDS by now
+    constexpr int set = P == 2 ? decltype(odd)::value : 0;
+    if (j + P < count) load(j + P, set);
     // the next block's keys, before their first tile's loads
     const int k1 = w.from + (j / TB + 1) * kBlock;
-    if (j % TB == TB - 3 && k1 < w.to) {
+    if (j % TB == TB - P - 2 && k1 < w.to) {
       put_rows(a, w, k1, h.page, &kb[(j / TB + 1) % 2]);
       put_keys<Q8>(a, w, rs, h, &kb[(j / TB + 1) % 2]);
       if (k1 + kBlock < w.to) {
@@ -990,8 +994,12 @@ __global__ __launch_bounds__(kThreads, R == 1 ? 3 : 2) void attn_tree_many_kerne
         }
       }
     }
-    if (j + 1 < count) store(j + 1);
+    if (j + 1 < count) store(j + 1, P == 2 ? 1 - set : 0);
     __syncthreads();
+  };
+  for (int j = 0; j < count; j += 2) {
+    turn(j, std::integral_constant<int, 0>{});
+    if (j + 1 < count) turn(j + 1, std::integral_constant<int, 1>{});
   }
   if (idle) return;
   if (sp.last) put_out<KIND, DQK, DV, R>(a, w, w0, head, q, acc);
