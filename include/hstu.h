@@ -401,9 +401,11 @@ hstu_status_t hstu_rotary_frequencies(int32_t rot_dim, double base,
 /* q_out, k_out (dense [T][h][d_qk]) = q, k (rows at q_stride / k_stride)
  * turned by their positions.  positions: int64 [T], or NULL: the token's
  * index in its sequence, at most n_h (the position rule of the candidates;
- * num_targets NULL: none), for which seq_offsets is needed; otherwise
- * seq_offsets and num_targets are not read.  Either of q and k may be NULL
- * together with its output.  inv_freq: rot_dim / 2 doubles in device memory.
+ * num_targets NULL: none), for which seq_offsets is needed (rows behind the
+ * last sequence are not written); otherwise seq_offsets and num_targets are not
+ * read.  Either of q and k may be NULL together with its output; an output may
+ * be its dense input.  inv_freq: rot_dim / 2 doubles in device memory.  At most
+ * 2^31 - 1 tokens.
  * p: total_tokens, num_heads, d_qk, dtype and, without positions, num_seqs
  * matter.  Deterministic; a row's bits do not depend on the other rows. */
 hstu_status_t hstu_rotary_fwd(const hstu_problem_t* p, const int64_t* seq_offsets,
@@ -507,7 +509,8 @@ hstu_status_t hstu_cache_validate(const hstu_problem_t* p, const hstu_cache_t* c
  *   out_i = (1/N) (sum_{j < n_b} SiLU(q_i . kc_j + rab(j - p_i, t_i - tc_j)) vc_j
  *                + sum_{j on i's way} SiLU(q_i . k_j + rab(p_j - p_i, t_i - t_j)) v_j)
  * with rab(x, dt) = rab_pos[N-1 + x] + rab_time[bkt(dt)], positions further
- * back than N - 1 taking rab_pos[0].  A chain (parents i - 1) of one token or
+ * back than N - 1 taking rab_pos[0].  Entries of the tables below -6e37 (the
+ * type's lowest value, -infinity) mask: the weight is 0.  A chain (parents i - 1) of one token or
  * several gives the outputs that hstu_attn_fwd gives the last tokens of a
  * sequence, but for the cache's rounding.  Cached tokens on a page outside the
  * pool, and past max_pages * page_size, are left out.  Drafted keys and values

@@ -613,6 +613,9 @@ int cache_kind(const hstu_cache_t* c) {
                                        : kCacheInt8;
 }
 
+// Workgroups of 256 threads that a launch can have, less what its rounding adds.
+constexpr int64_t kMaxBlocks = (1 << 24) - (1 << 10);
+
 hstu_status_t check_draft(int32_t max_draft) {
   static_assert(kMaxDraft == HSTU_MAX_DRAFT, "the header's limit is the kernels'");
   if (max_draft < 1)
@@ -630,8 +633,8 @@ hstu_status_t tree_plan(const hstu_problem_t* p, const hstu_cache_t* c, int32_t 
   if (cap > (int64_t)1 << 30)
     return fail(HSTU_ERR_UNSUPPORTED, "a page table for more than 2^30 tokens is not supported");
   *sp = tree_split(p->num_seqs, p->total_tokens, p->num_heads, p->max_seq_len, max_draft, cap);
-  if ((int64_t)p->num_seqs * sp->row_blocks * sp->chunks * p->num_heads > INT32_MAX ||
-      (int64_t)p->num_seqs * max_draft > INT32_MAX)
+  if ((int64_t)p->num_seqs * sp->row_blocks * sp->chunks * p->num_heads > kMaxBlocks ||
+      (int64_t)p->num_seqs * ((max_draft + sp->per - 1) / sp->per) > kMaxBlocks)
     return fail(HSTU_ERR_UNSUPPORTED, "%d sequences of %d drafted tokens over %lld cached ones",
                 p->num_seqs, max_draft, (long long)cap);
   *bytes = align_up(sizeof(float) * (size_t)sp->chunks * (size_t)p->total_tokens * p->num_heads *
@@ -799,6 +802,8 @@ hstu_status_t hstu_tree_positions(int32_t num_seqs, int64_t total_tokens, int32_
   try {
     if (num_seqs < 1) return fail(HSTU_ERR_INVALID_ARGUMENT, "num_seqs must be >= 1");
     if (total_tokens < 0) return fail(HSTU_ERR_INVALID_ARGUMENT, "total_tokens must be >= 0");
+    if (num_seqs > kMaxBlocks)
+      return fail(HSTU_ERR_UNSUPPORTED, "positions of %d sequences", num_seqs);
     HSTU_TRY(check_draft(max_draft));
     if (!seq_offsets) return fail(HSTU_ERR_INVALID_ARGUMENT, "seq_offsets is NULL");
     if (total_tokens == 0) return ok();

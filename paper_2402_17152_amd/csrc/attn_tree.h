@@ -47,6 +47,11 @@ constexpr int kBlock = 256;       // keys whose scales, times and pages are held
 constexpr int kWindow = 512;      // entries of rab_pos that are held at most
 constexpr float kNegLog2e = -kLog2e;
 
+// An entry of the bias tables.  The lowest ones, the type's lowest value and -inf among
+// them, are masks: held this far from the end of the range their sums and products
+// stay finite, and SiLU is 0 there.
+__device__ __forceinline__ float entry(float x) { return x < -6e37f ? -6e37f : x; }
+
 // What is known of 64 keys: each row's time bucket is the same for all; the time
 // differences fit 32 bits; all of the first, the second 32 keys are there.
 enum { kOneBucket = 1, kNear = 2, kWhole = 4 };
@@ -303,7 +308,7 @@ __device__ __forceinline__ void put_keys(const TreeArgs& a, const Part& w, const
 #pragma unroll
       for (int c = 0; c < 4; c++) {
         const int x = tid + e * kThreads - c;
-        if (x >= 0 && x < WIN) k->window[c][x] = h.pos[e] * kNegLog2e;
+        if (x >= 0 && x < WIN) k->window[c][x] = entry(h.pos[e]) * kNegLog2e;
       }
   // What the rows' times have in common with those of this wave's 64 keys:
   // |dt| is monotone in the key's time on either side of 0.
@@ -443,7 +448,7 @@ __device__ __forceinline__ void find_bias(const TreeArgs& a, const Part& w, cons
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
-        pos[i] = a.ja.rab_pos[max(0, N - 1 + k0 + at + i - w.n_b - depth[m])] * kNegLog2e;
+        pos[i] = entry(a.ja.rab_pos[max(0, N - 1 + k0 + at + i - w.n_b - depth[m])]) * kNegLog2e;
     }
 #pragma unroll
     for (int i = 0; i < 8; i++) bv[m][i / 4][i % 4] = pos[i] + rows.rtime[bucket[i]];
@@ -519,7 +524,7 @@ __device__ __forceinline__ void put_out(const TreeArgs& a, const Part& w, int w0
   typedef __bf16 bv __attribute__((ext_vector_type(NC)));
   const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
   const int N = a.ja.max_seq_len;
-  const float bias = a.ja.rab_pos[N - 1] + a.ja.rab_time[0];  // of a token and itself
+  const float bias = entry(a.ja.rab_pos[N - 1]) + entry(a.ja.rab_time[0]);  // of a token and itself
   const float inv = 1.0f / (float)N;
 #pragma unroll
   for (int m = 0; m < R; m++) {
@@ -648,7 +653,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_few_kernel(const TreeAr
   for (int m = 0; m < R; m++)
 #pragma unroll
     for (int c = 0; c < NC; c++) acc[m][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  rs.rtime[tid] = bucket_bias * kNegLog2e;
+  rs.rtime[tid] = entry(bucket_bias) * kNegLog2e;
   if (tid < 16 * R) rs.time[tid] = row_time;
   int depth[R];
   find_depths<true, R>(a, &w, 0, parent, nullptr, depth);
@@ -836,7 +841,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tree_many_kernel(const TreeA
   const float bucket_bias = tid < a.ja.num_buckets ? a.ja.rab_time[tid] : 0.0f;
   const int64_t row_time = tid < w.rows ? a.ja.timestamps[w.o + w.r0 + tid] : 0;
   const int64_t parent = a.parents && lane < w.r0 + w.rows ? a.parents[w.o + lane] : -1;
-  rs.rtime[tid] = bucket_bias * kNegLog2e;
+  rs.rtime[tid] = entry(bucket_bias) * kNegLog2e;
   if (tid < 64 * R) rs.time[tid] = row_time;
   // Tile j of the chunk: loads into one of P sets of registers, then into LDS.
   const int count = (w.to - w.from + T - 1) / T;

@@ -96,14 +96,14 @@ __device__ __forceinline__ void add8(float* x, u32x4 v, float w) {
 // of a workgroup share a row and head (`waves` 4).
 template <int DQK, int DV, typename Forest>
 __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
-                                                               const TreeSplit sp, int per,
-                                                               int waves) {
+                                                               const TreeSplit sp) {
   constexpr int LK = DQK / 8, LV = DV / 8;  // lanes of a K row, of a V row
   extern __shared__ short space[];
   __shared__ float score[kThreads / 64][64];
   __shared__ float rest[kThreads / 64 - 1][DV];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int H = a.ja.num_heads;
+  const int per = sp.per, waves = sp.waves;
   const int blocks = (a.max_draft + per - 1) / per;
   const int b = blockIdx.x / blocks, r0 = blockIdx.x % blocks * per;
   const int64_t o = a.ja.seq_offsets[b];
@@ -180,8 +180,9 @@ __global__ __launch_bounds__(kThreads) void tree_finish_kernel(const TreeArgs a,
         const int here = min(64, count - w0), mine = min(lane, here - 1);
         const int node = above(w0 + mine);
         const float bias =
-            a.ja.rab_pos[max(0, N - 1 - (w0 + mine))] +
-            a.ja.rab_time[time_bucket64(time - forest.time(a, o, node), a.ja.num_buckets)];
+            tree::entry(a.ja.rab_pos[max(0, N - 1 - (w0 + mine))]) +
+            tree::entry(a.ja.rab_time[time_bucket64(time - forest.time(a, o, node),
+                                                    a.ja.num_buckets)]);
 #pragma unroll 4
         for (int y0 = 0; y0 < here; y0 += 64 / LK) {
           float k[8] = {};
@@ -269,6 +270,10 @@ TreeSplit tree_split(int32_t num_seqs, int64_t total_tokens, int32_t num_heads, 
   const int64_t chunks = std::max((int64_t)1, std::min(most, (kWanted + base / 2) / base));
   sp.chunk_len = (int32_t)((most + chunks - 1) / chunks * tree::kBlock);
   sp.chunks = (int32_t)((cap + sp.chunk_len - 1) / sp.chunk_len);
+  // The finish: four waves for a row and head where there are many chunks, else a wave
+  // each, and a workgroup takes one row while there are few of them.
+  sp.waves = sp.chunks > 16 ? 4 : 1;
+  sp.per = sp.waves == 4 || total_tokens < 4096 ? 1 : total_tokens < 8192 ? 2 : 4;
   return sp;
 }
 
@@ -277,18 +282,14 @@ hipError_t launch_attn_tree(const TreeArgs& a, const TreeSplit& sp, int kind, hi
                  : kind == kCacheE4m3 ? tree::launch_e4m3(a, sp, s)
                                       : tree::launch_int8(a, sp, s);
   if (e != hipSuccess || sp.last) return e;
-  // Rows of a workgroup: one, while there are few of them.
-  const int waves = sp.chunks > 16 ? 4 : 1;
-  const int64_t T = a.ja.total_tokens;
-  const int per = waves == 4 || T < 4096 ? 1 : T < 8192 ? 2 : 4;
-  const dim3 grid((unsigned)((int64_t)a.ja.num_seqs * ((a.max_draft + per - 1) / per)),
-                  waves == 4 ? (unsigned)a.ja.num_heads : 1u);
+  const dim3 grid((unsigned)((int64_t)a.ja.num_seqs * ((a.max_draft + sp.per - 1) / sp.per)),
+                  sp.waves == 4 ? (unsigned)a.ja.num_heads : 1u);
   size_t space = 0;
   if (a.parents && a.max_draft > 64)
     for (int l = 0; l == 0 || 1 << l < a.max_draft; l++)
       space += (size_t)a.max_draft * sizeof(short);
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), space, s, a, sp, per, waves);
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), space, s, a, sp);
     return hipGetLastError();
   };
 #define HSTU_FINISH(DQK, DV)                                                        \

@@ -336,6 +336,8 @@ struct TreeSplit {
   int32_t hg;         // heads a workgroup takes: 1, 2 or 4
   int32_t rows;       // drafted rows it takes
   int32_t row_blocks;
+  int32_t per;        // drafted rows a workgroup of the finish takes
+  int32_t waves;      // of it for a row and head: 1 or 4
   int32_t last;       // outputs, not partial ones: one chunk, and no node sees another
 };
 // The split for these sizes, part left null.

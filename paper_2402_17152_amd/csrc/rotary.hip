@@ -8,6 +8,8 @@
 // sine and cosine: a position of 2^20 leaves an error of 2^-33 turns) and then
 // walks the rows of all heads of Q and K, neighbouring lanes on neighbouring
 // features.
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace hstu {
@@ -33,8 +35,12 @@ template <typename E, int W>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
   __shared__ float2 turn[kPairsLds];
   __shared__ double pos[kMaxTokens];
-  const int64_t t0 = (int64_t)blockIdx.x * a.per;
-  const int n = (int)min((int64_t)a.per, a.total_tokens - t0);
+  // a dimension of a grid holds 2^24 such workgroups
+  const int64_t t0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.per;
+  int64_t end = a.total_tokens;
+  if (!a.positions) end = min(end, a.seq_offsets[a.num_seqs]);
+  const int n = (int)min((int64_t)a.per, end - t0);
+  if (n <= 0) return;
   if (a.positions) {
     if ((int)threadIdx.x < n) pos[threadIdx.x] = (double)a.positions[t0 + threadIdx.x];
   } else {
@@ -105,7 +111,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
 template <typename E, int W>
 hipError_t run(const RotaryArgs& a, hipStream_t s) {
   const int64_t blocks = (a.total_tokens + a.per - 1) / a.per;
-  hipLaunchKernelGGL((rotary_kernel<E, W>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  const int64_t width = std::min(blocks, (int64_t)1 << 20);
+  hipLaunchKernelGGL((rotary_kernel<E, W>),
+                     dim3((unsigned)width, (unsigned)((blocks + width - 1) / width)),
+                     dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -172,6 +172,47 @@ def test_positions_of_the_batch(lengths):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [70, 5000])
+def test_rows_behind_the_last_sequence(T):
+    """A batch padded behind its last sequence: the padding is left as it was."""
+    q, _ = _rows(T, 2, 32, torch.bfloat16, 8, strided=True)
+    f = torch.from_numpy(hstu.hstu_rotary_frequencies(32)).cuda()
+    n = T // 2 + 1
+    offs = torch.tensor([0, 3, n]).cuda()
+    out = torch.full((T, 2, 32), 7.0, device="cuda").bfloat16()
+    hstu.hstu_rotary_fwd(q, None, f, seq_offsets=offs, out=(out, None))
+    assert (out[n:] == 7).all()
+    want, _ = hstu.hstu_rotary_fwd(q[:n], None, f, seq_offsets=offs)
+    assert torch.equal(out[:n], want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_in_place(interleaved):
+    q, k = _rows(130, 3, 64, torch.bfloat16, 6, strided=False)
+    q, k = q.contiguous(), k.contiguous()
+    f = torch.from_numpy(hstu.hstu_rotary_frequencies(40)).cuda()
+    pos = torch.arange(130).cuda()
+    want = hstu.hstu_rotary_fwd(q, k, f, positions=pos, interleaved=interleaved)
+    hstu.hstu_rotary_fwd(q, k, f, positions=pos, interleaved=interleaved, out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+@pytest.mark.gpu
+def test_more_workgroups_than_a_row_of_the_grid():
+    """2^25 + 33 rows of 32 features (2 GB): the last workgroups lie in the grid's
+    second row."""
+    T = (1 << 25) + 33
+    x = torch.ones(1, 1, 1, dtype=torch.bfloat16, device="cuda").expand(T, 1, 32).contiguous()
+    f = torch.from_numpy(hstu.hstu_rotary_frequencies(32)).cuda()
+    pos = torch.arange(T, device="cuda")
+    out, _ = hstu.hstu_rotary_fwd(x, None, f, positions=pos)
+    for lo in (0, (1 << 25) - 40, T - 70):
+        want, _ = hstu.hstu_rotary_fwd(x[lo:lo + 70], None, f, positions=pos[lo:lo + 70])
+        assert torch.equal(out[lo:lo + 70], want)
+
+
+@pytest.mark.gpu
 def test_features_behind_the_turned_ones_keep_their_bits():
     x = torch.randn(9, 2, 64, device="cuda").bfloat16()
     x[:, :, 33] = float("nan")

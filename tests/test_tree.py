@@ -73,6 +73,17 @@ def test_workspace_and_positions_refusals():
         assert st == status
 
 
+def test_more_workgroups_than_a_launch_has():
+    c = hstu.CacheDesc(num_pages=8, page_size=256, max_pages=1, dtype=hstu.HSTU_CACHE_INT8)
+    p = _problem(num_seqs=(1 << 24) // 16, num_heads=64)
+    assert hstu.lib.hstu_attn_fwd_tree_workspace_bytes(ctypes.byref(p), ctypes.byref(c), 1) == 0
+    assert "sequences of 1 drafted" in hstu.hstu_last_error()
+    p = _problem(num_seqs=1 << 20, num_heads=1)
+    assert hstu.lib.hstu_attn_fwd_tree_workspace_bytes(ctypes.byref(p), ctypes.byref(c), 64) == 0
+    st = hstu.lib.hstu_tree_positions(1 << 24, 10, 8, P(FAKE), None, None, P(FAKE), None)
+    assert st == 2 and "sequences" in hstu.hstu_last_error()
+
+
 def test_binding_refusals(monkeypatch):
     monkeypatch.setattr(hstu, "_raw_device", lambda: 0)
     cache = hstu.PagedCache(torch.zeros(4, 2, 16, 32).bfloat16(),
@@ -330,6 +341,28 @@ def test_infinities_in_the_cache_follow_the_formula():
     out = x.run()
     assert torch.equal(out[:5], clean[:5])
     assert torch.isnan(out[5:, 1]).all() and torch.isfinite(out[5:, 0].float()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("low", [torch.finfo(torch.float32).min, float("-inf")])
+@pytest.mark.parametrize("nodes,hist,N", [((1, 3), (40, 700), None), ((20, 9), (70, 300), None),
+                                          ((40, 64), (100, 600), None), ((200, 7), (300, 20), None),
+                                          ((300, 1), (260, 5), 2000)])
+def test_tables_that_mask(nodes, hist, N, low):
+    """Entries of the lowest value, or -inf, in either table or in both: weights of
+    0.  The reference takes -200 for them, for which SiLU is below 2^-200."""
+    x = Batch(hist, nodes, 2, 32, 32, "int8", 32, "comb", N=N, seed=13, scale=0.5)
+    for t in (x.rab_pos, x.rab_time):
+        t[torch.rand(t.shape, generator=torch.Generator().manual_seed(14)) < 0.4] = -200.0
+    x.rab_pos[x.N - 1] = 0.1  # a token and itself: not masked by the position
+    x.rab_time[0] = -200.0    # but by the time
+    for name in ("rab_pos", "rab_time"):
+        t = getattr(x, name).cuda()
+        x.dev[name] = torch.where(t == -200.0, torch.full_like(t, low), t)
+    x.check(x.run())
+    for name in ("rab_pos", "rab_time"):  # everything masked
+        x.dev[name] = torch.full_like(x.dev[name], low)
+    assert (x.run() == 0).all() and (x.run(parents=False) == 0).all()
 
 
 @pytest.mark.gpu
