@@ -93,16 +93,17 @@ __device__ __forceinline__ uint2 quantise(const float* x, uint32_t top, float* s
     // big = 1.m * 2^x: 448 = 1.75 * 2^8, so the exponent is x - 8, one more for m > 0.75.
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
     e = min(e, 119);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);  // 2^-e; e >= -109
 #pragma unroll
     for (int i = 0; i < 2; i++) {
       float y[4];
 #pragma unroll
       for (int b = 0; b < 4; b++)
-        y[b] = fminf(fmaxf(ldexpf(x[4 * i + b], -e), -448.0f), 448.0f);
+        y[b] = __builtin_amdgcn_fmed3f(x[4 * i + b] * inv, -448.0f, 448.0f);
       int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
       w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], p, true);
     }
-    *scale = ldexpf(1.0f, e);
+    *scale = __uint_as_float((uint32_t)(127 + e) << 23);
   }
   return uint2{w[0], w[1]};
 }
@@ -247,7 +248,7 @@ __device__ __forceinline__ void encode(const Eight<E>& e, uint32_t* w, float* sc
 }
 
 template <typename E, int KIND, int DQK, int DV>
-__global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a) {
+__global__ __launch_bounds__(kThreads, 5) void cache_write_kernel(const CacheArgs a) {
   using Tl = Tile<KIND, DV>;
   constexpr int CB = Tl::CB, FP = Tl::FP;
   constexpr int LK = DQK / 8, LV = DV / 8;                              // lanes of a row
