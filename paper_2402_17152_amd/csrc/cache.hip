@@ -7,7 +7,7 @@
 // head.  d / 8 neighbouring lanes share a row, so that its largest magnitude
 // takes a few lane exchanges.  K rows go where they belong as they are; V goes
 // through LDS, because a page holds a feature's keys side by side.  25000 tokens
-// of 4 heads of 128, e4m3: written in 22.7 us (3.4 TB/s), read back in 16.1 (4.8;
+// of 4 heads of 128, e4m3: written in 22.6 us (3.4 TB/s), read back in 16.0 (4.8;
 // a large copy: 5.2); 8 users of 4096-8192, int8, read in 31.8 us (4.8 TB/s); a
 // token for each of 64 users: 9.4 and 4.8 us, a chain of dependent loads.
 #include "kernels.h"
@@ -247,6 +247,8 @@ __device__ __forceinline__ void encode(const Eight<E>& e, uint32_t* w, float* sc
   }
 }
 
+// Five waves a SIMD: what the registers of all its loads allow (six spill: 44 us against
+// 38 for writing and reading 25000 tokens).
 template <typename E, int KIND, int DQK, int DV>
 __global__ __launch_bounds__(kThreads, 5) void cache_write_kernel(const CacheArgs a) {
   using Tl = Tile<KIND, DV>;
