@@ -24,7 +24,7 @@
  *            comment says "host".  The library keeps no pointer after a
  *            call returns and allocates no device memory; scratch space
  *            comes from the caller's workspace (hstu_workspace_bytes).
- *            Outputs must not alias inputs.
+ *            Outputs must not alias inputs, unless a call says so.
  *   Layout   jagged, token-major: sequence b owns tokens
  *            [seq_offsets[b], seq_offsets[b+1]).  Q/K/V/U rows: row r of X
  *            starts at X + r * x_stride (in elements); inside a row the
@@ -37,7 +37,7 @@
  *            size <= 2^31, else HSTU_ERR_UNSUPPORTED).
  *   Streams  all work is enqueued on hip_stream (a hipStream_t, NULL =
  *            the null stream) and the call returns before it completes.
- *            Only hstu_validate synchronises.
+ *            Only hstu_validate and hstu_cache_validate synchronise.
  *   Errors   host-side argument checks run before any launch; on failure
  *            the call returns a non-zero hstu_status_t, sets
  *            hstu_last_error() and enqueues nothing.  A failed launch
@@ -55,8 +55,9 @@
  *            them, and the layer's dO, as two bf16 terms (hi + lo, about
  *            2^-17 relative instead of 2^-9).  Bias tables and their
  *            gradients are fp32; offsets and timestamps int64.
- *   Determinism  hstu_attn_fwd, hstu_layer_fwd, hstu_time_bucketize and
- *            hstu_complete_cumsum are bitwise deterministic, and so are
+ *   Determinism  hstu_attn_fwd, hstu_layer_fwd, hstu_time_bucketize,
+ *            hstu_complete_cumsum and the calls of rotary positions, the paged
+ *            cache and drafted tokens are bitwise deterministic, and so are
  *            dQ, dK and dV of hstu_attn_bwd (for HSTU_BF16, dQ is summed
  *            from per-key-block partials in a fixed order), dQ, dK and dV of
  *            hstu_layer_bwd for HSTU_F32 and for HSTU_BF16 with d_qk, d_v <=

@@ -426,6 +426,56 @@ def test_captured_and_replayed():
 
 
 @pytest.mark.gpu
+def test_captured_steps():
+    """A serving step as one graph: positions, rotary, attention, then all drafted
+    tokens (chains) enter the cache; each replay stands behind the one before."""
+    lens, drafts, h, d, N = (70, 0, 31), (3, 16, 5), 2, 64, 300
+    g = torch.Generator().manual_seed(30)
+    T = sum(drafts)
+    z = torch.randn(T, 3 * h * d, generator=g).bfloat16().cuda()
+    q, k, v = (z[:, i * h * d:(i + 1) * h * d].unflatten(1, (h, d)) for i in range(3))
+    ts = torch.randint(0, 1 << 30, (T,), generator=g).cuda()
+    rp, rt = (0.1 * torch.randn(n, generator=g).cuda() for n in (2 * N - 1, 32))
+    offs = torch.tensor(np.concatenate([[0], np.cumsum(drafts)])).cuda()
+    par = torch.tensor([i - 1 for n in drafts for i in range(n)]).cuda()
+    freq = torch.from_numpy(hstu.hstu_rotary_frequencies(d)).cuda()
+    n_new = torch.tensor(drafts).cuda()
+
+    def fresh():
+        cache = hstu.alloc_cache(30, 16, h, d, d, 3, 10, torch.int8)
+        cache.page_table.copy_(torch.arange(30).view(3, 10))
+        cache.lengths.copy_(torch.tensor(lens))
+        ho = torch.tensor(np.concatenate([[0], np.cumsum(lens)])).cuda()
+        gen = torch.Generator().manual_seed(31)
+        x = torch.randn(sum(lens), h, d, generator=gen).bfloat16().cuda()
+        hstu.hstu_cache_write(x, x, torch.arange(sum(lens)).cuda(), ho, cache)
+        return cache
+
+    def step(cache):
+        pos = hstu.hstu_tree_positions(par, offs, cache.lengths, T, 16)
+        qr, kr = hstu.hstu_rotary_fwd(q, k, freq, positions=pos)
+        out = hstu.hstu_attn_fwd_tree(qr, kr, v, offs, ts, cache, rp, rt, N, 16, parents=par)
+        hstu.hstu_cache_write(kr, v, ts, offs, cache, starts=cache.lengths)
+        cache.lengths.add_(n_new)
+        return out
+    eager, held = fresh(), fresh()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(held)
+    for _ in range(4):
+        z.mul_(0.9)
+        want = step(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(held.lengths, eager.lengths)
+    at = torch.tensor(np.concatenate([[0], np.cumsum(eager.lengths.cpu().numpy())])).cuda()
+    n = int(at[-1])
+    for a, b in zip(hstu.hstu_cache_read(held, at, n), hstu.hstu_cache_read(eager, at, n)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_positions():
     x = Batch((3, 100, 0, 7), (1024, 0, 77, 5), 1, 32, 32, shape="comb", seed=15)
     want = np.concatenate([h + ref.depths(p)[0] for h, p in zip(x.hist, x.par)])
