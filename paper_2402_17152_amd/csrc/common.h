@@ -71,23 +71,6 @@ __device__ __forceinline__ int64_t readlane64(int64_t v, int lane) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The sequence that owns packed row t: the last b in [0, B) with offs[b] <= t
-// (0 for t < offs[0]).  t is the same in all 64 lanes, which probe 64 places
-// at a time: one dependent load for B <= 64, two for B <= 4096.
-__device__ __forceinline__ int find_seq(const int64_t* __restrict__ offs, int B, int64_t t) {
-  const int lane = __lane_id();
-  int lo = 0, n = B;
-  while (n > 1) {
-    const int step = (n + 63) / 64;
-    const int at = lane * step;
-    const uint64_t below = __ballot(at < n && offs[lo + (at < n ? at : 0)] <= t);
-    const int last = below ? 63 - __builtin_clzll(below) : 0;
-    lo += last * step;
-    n = min(step, n - last * step);
-  }
-  return lo;
-}
-
 // Packs two floats into two bf16 (round to nearest even) in one dword.
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   bf16x2 r;

@@ -31,6 +31,23 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ void from_f32(float x, uint16_t& o) { o = f32_to_bf16_bits(x); }
 __device__ __forceinline__ void from_f32(float x, float& o) { o = x; }
 
+// The sequence that owns packed row t: the last b in [0, B) with offs[b] <= t
+// (0 for t < offs[0]).  t is the same in all 64 lanes, which probe 64 places
+// at a time: one dependent load for B <= 64, two for B <= 4096.
+__device__ __forceinline__ int find_seq(const int64_t* __restrict__ offs, int B, int64_t t) {
+  const int lane = __lane_id();
+  int lo = 0, n = B;
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int at = lane * step;
+    const uint64_t below = __ballot(at < n && offs[lo + (at < n ? at : 0)] <= t);
+    const int last = below ? 63 - __builtin_clzll(below) : 0;
+    lo += last * step;
+    n = min(step, n - last * step);
+  }
+  return lo;
+}
+
 // E: storage type (bf16 bits or fp32); W: pairs a thread turns at once, the
 // width of its two loads and two stores.
 template <typename E, int W>
